@@ -510,3 +510,20 @@ def kvx_pd_evaluate(problem: kvx_pd_problem, side: int, dp: int, tp: int, pp: in
     _check(_lib.kvx_pd_evaluate(ctypes.byref(problem), side, dp, tp, pp, ep, batch,
                                 ctypes.byref(out)))
     return out
+
+
+# The decode operators over the cache (include/kvx_ops.h) are bound in
+# operators.py, which is read at the first use of one of its names.
+_OPERATOR_NAMES = frozenset((
+    "OPERATORS", "OPS_VERSION", "kvx_append", "kvx_attend", "kvx_attend_workspace", "kvx_batch",
+    "kvx_cache", "kvx_commit", "kvx_evict", "kvx_ops_version", "kvx_rope", "kvx_scores",
+    "kvx_weigh", "make_batch", "make_cache", "make_rope", "make_scores"))
+
+
+def __getattr__(name):
+    if name not in _OPERATOR_NAMES:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import operators
+    for n in _OPERATOR_NAMES:
+        globals()[n] = getattr(operators, n)
+    return globals()[name]

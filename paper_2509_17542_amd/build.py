@@ -22,7 +22,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-ffp-contract=off", "-I", INCL
 DEVICE = ["-x", "hip", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",
           "-packed-fp32-ops"]
 SOURCES = [("kvx_kernels.hip", True), ("kvx_plan.cpp", False), ("kvx_pipe.cpp", False),
-           ("kvx_pd.cpp", False)]
+           ("kvx_pd.cpp", False), ("kvx_ops.cpp", False), ("kvx_slots.hip", True),
+           ("kvx_attend.hip", True)]
 
 
 def build(verbose: bool = False) -> str:

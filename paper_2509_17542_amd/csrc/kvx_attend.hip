@@ -1,0 +1,190 @@
+// gfx950 kernels of attention over the paged cache (kvx_attend) and of the
+// slots' accumulated weights (kvx_weigh).
+#include <hip/hip_runtime.h>
+
+#include "kvx_ops_dev.h"
+
+namespace kvx {
+namespace {
+
+template <int kCache>
+constexpr bool is8() { return kCache == KVX_FP8_E4M3FN || kCache == KVX_FP8_E5M2; }
+
+template <int kCache>
+__device__ __forceinline__ float element(const char* row, int i)
+{
+    if constexpr (is8<kCache>())
+        return value8<kCache == KVX_FP8_E5M2, 0>(reinterpret_cast<const uint8_t*>(row)[i]);
+    else
+        return value16<kCache == KVX_BF16>(reinterpret_cast<const uint16_t*>(row)[i]);
+}
+
+// Whether token i of request r sees slot j, and the distance between them.
+__device__ __forceinline__ bool visible(const AttendArgs& a, const Request& rq, int r, int i, int j,
+                                        int& distance)
+{
+    const int tok = rq.first + i;
+    const int qp = a.b.positions ? a.b.positions[tok] : rq.ctx + i;
+    const int kp = j >= rq.ctx && a.b.positions ? a.b.positions[rq.first + j - rq.ctx] : j;
+    distance = qp - kp;
+    if (j >= rq.total) return false;
+    if (a.prefix && j < a.prefix[r]) return true;
+    bool see = true;
+    if (j >= rq.ctx) {
+        const int k = j - rq.ctx;
+        see = a.b.tree ? (a.b.tree[int64_t(tok) * a.b.tree_stride + (k >> 6)] >> (k & 63)) & 1
+                       : k <= i;
+    }
+    return see && (a.window <= 0 || distance < a.window);
+}
+
+__device__ __forceinline__ float score(const AttendArgs& a, float dot, int head, int distance)
+{
+    float x = dot * a.scale;
+    if (a.softcap > 0.0f) x = a.softcap * tanhf(x / a.softcap);
+    if (a.slopes) x -= a.slopes[head] * static_cast<float>(abs(distance));
+    return x;
+}
+
+// One wave per (token, query head): 64 slots at a time, a lane to each.
+template <bool kBf16, int kCache>
+__global__ void __launch_bounds__(64) kvx_attend_kernel(const AttendArgs a)
+{
+    __shared__ float qs[256], ps[64];
+    const int t = int(blockIdx.x) / a.q_heads, head = int(blockIdx.x) % a.q_heads;
+    const int lane = threadIdx.x, D = a.c.dim;
+    const int g = head / a.group;
+    uint16_t* out = a.out + t * a.out_stride + int64_t(head) * D;
+    const int r = request_at(a.b.starts, a.c.num_requests, t);
+    Request rq = {};
+    int i = 0;
+    if (r >= 0 && r < a.c.num_requests) {
+        rq = request_of(a.c, a.b, r);
+        i = t - rq.first;
+    }
+    for (int d = lane; d < D; d += 64)
+        qs[d] = value16<kBf16>(a.q[t * a.q_stride + int64_t(head) * D + d]);
+    __syncthreads();
+    float m = -INFINITY, l = 0.0f, o[4] = {};
+    const char* kb = a.c.base;
+    const char* vb = a.c.base + a.c.plane_bytes;
+    for (int j0 = 0; j0 < rq.total; j0 += 64) {
+        const int j = j0 + lane;
+        float x = -INFINITY, vs = 0.0f;
+        int64_t row = -1;
+        int dist;
+        if (j < rq.total && i < rq.n && visible(a, rq, r, i, j, dist)) row = slot_row(a.c, r, j);
+        if (row >= 0) {
+            const char* k = kb + (row + g) * a.c.row_bytes;
+            float dot = 0.0f;
+            for (int d = 0; d < D; ++d) dot = __builtin_fmaf(qs[d], element<kCache>(k, d), dot);
+            if constexpr (is8<kCache>()) {
+                dot *= a.c.scales[row + g];
+                vs = a.c.scales[a.c.plane_scales + row + g];
+            }
+            x = score(a, dot, head, dist);
+        }
+        float mt = x;
+        for (int s = 32; s; s >>= 1) mt = fmaxf(mt, __shfl_xor(mt, s));
+        const float mn = fmaxf(m, mt);
+        const float alpha = mn == -INFINITY ? 1.0f : __expf(m - mn);
+        const float p = x == -INFINITY ? 0.0f : __expf(x - mn);
+        float sum = p;
+        for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
+        l = l * alpha + sum;
+        m = mn;
+        for (int k = 0; k < 4; ++k) o[k] *= alpha;
+        __syncthreads();
+        ps[lane] = is8<kCache>() ? p * vs : p;
+        __syncthreads();
+        for (int jj = 0; jj < 64; ++jj) {
+            const int64_t rj = __shfl(row, jj);
+            if (rj < 0) continue;
+            const char* v = vb + (rj + g) * a.c.row_bytes;
+            for (int k = 0; k < 4; ++k)
+                if (lane + 64 * k < D)
+                    o[k] = __builtin_fmaf(ps[jj], element<kCache>(v, lane + 64 * k), o[k]);
+        }
+    }
+    for (int k = 0; k < 4; ++k)
+        if (lane + 64 * k < D)
+            out[lane + 64 * k] = uint16_t(bits16<kBf16>(l > 0.0f ? o[k] / l : 0.0f));
+    if (a.lse && lane == 0)
+        a.lse[int64_t(t) * a.q_heads + head] = l > 0.0f ? m + logf(l) : -INFINITY;
+}
+
+// One wave per (request, KV head, 64 slots): a lane to each slot.
+template <bool kBf16, int kCache>
+__global__ void __launch_bounds__(64) kvx_weigh_kernel(const AttendArgs a, int tiles)
+{
+    const int lane = threadIdx.x, D = a.c.dim;
+    const int g = (int(blockIdx.x) / tiles) % a.c.hd, r = int(blockIdx.x) / tiles / a.c.hd;
+    const Request rq = request_of(a.c, a.b, r);
+    const int j = int(blockIdx.x) % tiles * 64 + lane;
+    if (j >= rq.total) return;
+    const int64_t row = slot_row(a.c, r, j);
+    float w = 0.0f;
+    if (row >= 0) {
+        const char* k = a.c.base + (row + g) * a.c.row_bytes;
+        for (int i = 0; i < rq.n; ++i) {
+            int dist;
+            if (!visible(a, rq, r, i, j, dist)) continue;
+            for (int h = g * a.group; h < (g + 1) * a.group; ++h) {
+                const uint16_t* q = a.q + int64_t(rq.first + i) * a.q_stride + int64_t(h) * D;
+                float dot = 0.0f;
+                for (int d = 0; d < D; ++d)
+                    dot = __builtin_fmaf(value16<kBf16>(q[d]), element<kCache>(k, d), dot);
+                if constexpr (is8<kCache>()) dot *= a.c.scales[row + g];
+                const float lse = a.lse[int64_t(rq.first + i) * a.q_heads + h];
+                if (lse > -INFINITY) w += __expf(score(a, dot, h, dist) - lse);
+            }
+        }
+    }
+    float* out = a.weights + (int64_t(r) * a.c.hd + g) * a.w_stride + j;
+    *out = j < rq.ctx ? *out + w : w;
+}
+
+template <bool kBf16, int kCache>
+int attend_as(const AttendArgs& a, void* stream)
+{
+    kvx_attend_kernel<kBf16, kCache><<<dim3(uint32_t(a.b.total_tokens) * a.q_heads), dim3(64), 0,
+                                       static_cast<hipStream_t>(stream)>>>(a);
+    return int(hipGetLastError());
+}
+
+template <bool kBf16, int kCache>
+int weigh_as(const AttendArgs& a, void* stream)
+{
+    const int tiles = (a.b.max_context + 63) / 64;
+    kvx_weigh_kernel<kBf16, kCache><<<dim3(uint32_t(tiles) * a.c.hd * a.c.num_requests), dim3(64), 0,
+                                      static_cast<hipStream_t>(stream)>>>(a, tiles);
+    return int(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_attend(const AttendArgs& a, int dtype, int cache_dtype, void*, void* stream)
+{
+    const bool bf = dtype == KVX_BF16;
+    switch (cache_dtype) {
+    case KVX_FP16: return attend_as<false, KVX_FP16>(a, stream);
+    case KVX_BF16: return attend_as<true, KVX_BF16>(a, stream);
+    case KVX_FP8_E4M3FN: return bf ? attend_as<true, KVX_FP8_E4M3FN>(a, stream) : attend_as<false, KVX_FP8_E4M3FN>(a, stream);
+    default: return bf ? attend_as<true, KVX_FP8_E5M2>(a, stream) : attend_as<false, KVX_FP8_E5M2>(a, stream);
+    }
+}
+
+int launch_weigh(const AttendArgs& a, int dtype, int cache_dtype, void* stream)
+{
+    const bool bf = dtype == KVX_BF16;
+    switch (cache_dtype) {
+    case KVX_FP16: return weigh_as<false, KVX_FP16>(a, stream);
+    case KVX_BF16: return weigh_as<true, KVX_BF16>(a, stream);
+    case KVX_FP8_E4M3FN: return bf ? weigh_as<true, KVX_FP8_E4M3FN>(a, stream) : weigh_as<false, KVX_FP8_E4M3FN>(a, stream);
+    default: return bf ? weigh_as<true, KVX_FP8_E5M2>(a, stream) : weigh_as<false, KVX_FP8_E5M2>(a, stream);
+    }
+}
+
+uint64_t attend_workspace(const kvx_cache&, const kvx_batch&, int32_t) { return 0; }
+
+}  // namespace kvx

@@ -1,0 +1,120 @@
+// Internal declarations shared by the host side of the decode operators
+// (kvx_ops.cpp) and their kernels (kvx_slots.hip, kvx_attend.hip).
+#pragma once
+
+#include <cstdint>
+
+#include "kvx_internal.h"
+#include "kvx_ops.h"
+
+namespace kvx {
+
+// One layer range of a cache as the kernels address it.  A plane is the pages
+// of one (layer, k/v): [num_blocks][block_size][hd][dim].
+struct CacheArgs {
+    char* base;                  // plane (layer0, k)
+    float* scales;               // its scales, NULL for 16-bit elements
+    const int32_t* table;
+    int64_t plane_bytes;         // bytes between planes
+    int64_t plane_scales;        // scales between planes
+    int64_t num_blocks;
+    int32_t bt_stride;
+    int32_t block_size;
+    int32_t hd;
+    int32_t dim;
+    int32_t row_bytes;           // dim x element size
+    int32_t row_slots;           // slots of a block-table row: bt_stride x block_size, cut to int32
+    int32_t num_requests;
+    int32_t pad;
+    FastDiv div_bs;              // by block_size
+};
+
+struct BatchArgs {
+    const int32_t* starts;
+    const int32_t* contexts;
+    const int32_t* positions;
+    const uint64_t* tree;
+    int32_t tree_stride;
+    int32_t total_tokens;
+    int32_t max_tokens;
+    int32_t max_context;
+};
+
+struct AppendArgs {
+    CacheArgs c;
+    BatchArgs b;
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    uint16_t* q_out;
+    int64_t q_stride, k_stride, v_stride, q_out_stride;
+    const float* inv_freq;
+    const int32_t* positions;    // [axes][N]
+    int32_t q_heads;
+    int32_t pairs;
+    int32_t interleaved;
+    int32_t sec_end[4];          // pairs below sec_end[a] belong to an axis <= a
+    int32_t lg_row;              // log2 of the lanes per head: a power of two >= dim / 8
+};
+
+struct EvictArgs {
+    CacheArgs c;
+    const int32_t* lens;
+    const float* weights;
+    float* weights_out;
+    int32_t* kept;
+    int32_t* new_lens;
+    int64_t w_stride;
+    int32_t max_len, budget, sink, recent;
+};
+
+struct CommitArgs {
+    const int32_t* contexts;
+    const int32_t* accepted;
+    const int32_t* counts;
+    int32_t* new_lens;
+    int32_t a_stride;
+    int32_t pad;
+};
+
+// Rows that move up inside their request: row first + i takes row first +
+// index[i], index ascending.
+struct MoveArgs {
+    CacheArgs c;
+    const int32_t* index;        // evict: [layer][request][head][stride]; commit: [request][stride]
+    int32_t stride;
+    int32_t num_layers;
+    // evict: rows of request r are min(lens[r], stride) where lens[r] > stride, else none;
+    // commit: new_lens[r] - contexts[r], from slot contexts[r] on
+    const int32_t* lens;
+    const int32_t* contexts;
+    const int32_t* new_lens;
+    int32_t max_len;
+    int32_t pad;
+};
+
+struct AttendArgs {
+    CacheArgs c;                 // base: the layer's k plane
+    BatchArgs b;
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;                  // weigh: read
+    float* weights;              // weigh
+    int64_t q_stride, out_stride, w_stride;
+    const float* slopes;
+    const int32_t* prefix;
+    float scale, softcap;
+    int32_t window;
+    int32_t q_heads;
+    int32_t group;
+};
+
+// Each enqueues its kernels on `stream` and returns a hipError_t value.
+int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream);
+int launch_evict(const EvictArgs& a, int num_layers, void* stream);
+int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void* stream);
+int launch_attend(const AttendArgs& a, int dtype, int cache_dtype, void* workspace, void* stream);
+int launch_weigh(const AttendArgs& a, int dtype, int cache_dtype, void* stream);
+uint64_t attend_workspace(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
+
+}  // namespace kvx

@@ -1,0 +1,498 @@
+// Attention of few query rows per KV head (one token, small trees) over the
+// paged cache: up to 16 or 32 rows, the tokens of a request times the query
+// heads of a KV head.
+//
+// Bound by reading K and V once.  A workgroup takes `chunk` slots of one request
+// and KV head; its 4 waves take 32 slots at a time in turn, each with all the
+// rows, and K and V go from memory to the matrix instructions' registers with no
+// stop in LDS:
+//   S^T = K Q^T   lane (slot, g) holds 8 elements of its slot's row: 16 bytes;
+//   O^T = V^T P^T lane (m, g) holds, for 8 slots, the DT elements m DT .. of the
+//                 row, so that 16 lanes read a row whole; element t of each is
+//                 the operand of the t-th product, whose 16 result rows are
+//                 the elements m DT + t.  The 8 slots are the ones whose
+//                 weights the lane holds, so neither P nor V crosses lanes; V's
+//                 16-bit pairs are put together by v_perm_b32.
+// Where a slot's row lies is looked up once per chunk into LDS.
+#include <hip/hip_runtime.h>
+
+#include "kvx_attend_dev.h"
+
+namespace kvx {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kWg = 64 * kWaves;
+constexpr int kTile = 32;           // slots of a wave's turn
+constexpr int kMaxChunk = 512;
+
+template <int kBytes>
+struct Words {
+    uint32_t w[kBytes / 4];
+};
+
+template <int kBytes>
+__device__ __forceinline__ Words<kBytes> load_words(const char* p)
+{
+    Words<kBytes> v;
+    if constexpr (kBytes == 4) {
+        v.w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (kBytes == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        v.w[0] = x.x, v.w[1] = x.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kBytes / 16; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4*>(p + 16 * i);
+            v.w[4 * i] = x.x, v.w[4 * i + 1] = x.y, v.w[4 * i + 2] = x.z, v.w[4 * i + 3] = x.w;
+        }
+    }
+    return v;
+}
+
+template <int kBytes>
+__device__ __forceinline__ Words<kBytes> no_words()
+{
+    Words<kBytes> v;
+#pragma unroll
+    for (int i = 0; i < kBytes / 4; ++i) v.w[i] = 0;
+    return v;
+}
+
+// One tile's K and V as a lane holds them.
+template <int kCodes, int DP>
+struct Tile {
+    static constexpr int kEl = kCodes == kCodes16 ? 2 : 1;
+    static constexpr int DT = DP / 16;
+    static constexpr int kVBytes = DT * kEl;
+    // K: pieces of 16 bytes, 8 elements or 16 codes
+    static constexpr int kPieces = DP * kEl / 64;
+    Words<16> k[2][kPieces];
+    Words<kVBytes> v[8];
+};
+
+// Registers decide how many waves a SIMD holds: O takes DP RT / 4, K and V up to
+// DP / 4 each.
+template <int DP, int RT>
+constexpr int kWavesPerSimd = DP >= 256 ? 1 : DP * RT >= 128 ? 2 : 3;
+
+template <bool kBf16, int kCodes, int DP, int RT>
+__global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_kernel(const AttendArgs a)
+{
+    using T = Tile<kCodes, DP>;
+    constexpr int DT = T::DT, kRows = 16 * RT;
+    constexpr bool k8 = kCodes != kCodes16;
+    constexpr bool kRef = k8 && !kBf16;             // fp16 weights take V's scale relative to one
+    constexpr int kKeyBytes = kMaxChunk * (k8 ? 20 : 12);
+    constexpr int kSlabBytes = 2 * kRows * DP * 4;
+    __shared__ __attribute__((aligned(16))) char smem[kKeyBytes > kSlabBytes ? kKeyBytes : kSlabBytes];
+    __shared__ float s_ml[kWaves][kRows][2];
+    int64_t* const s_off = reinterpret_cast<int64_t*>(smem);
+    int32_t* const s_pos = reinterpret_cast<int32_t*>(smem + kMaxChunk * 8);
+    float* const s_ks = reinterpret_cast<float*>(smem + kMaxChunk * 12);
+    float* const s_vs = reinterpret_cast<float*>(smem + kMaxChunk * 16);
+
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n16 = lane & 15, g = lane >> 4;
+    const int D = a.c.dim, G = a.group;
+    uint32_t u = blockIdx.x;
+    const int h = int(u % uint32_t(a.c.hd));
+    u /= uint32_t(a.c.hd);
+    const int split = int(u % uint32_t(a.splits)), r = int(u / uint32_t(a.splits));
+    const Request rq = request_of(a.c, a.b, r);
+    const int rows = rq.n * G;
+    if (rows == 0) return;
+    const Range rg = range_of(a, rq, r, 0, rq.n - 1);
+    const int v0 = split * a.chunk, v1 = min(v0 + a.chunk, rg.len);
+    float* const part_ml = a.part_ml + int64_t(split) * a.b.total_tokens * a.q_heads * 2;
+    if (a.splits > 1 && v0 >= v1) {
+        for (int i = tid; i < rows; i += kWg) {
+            const int tok = int(fast_div(uint32_t(i), a.div_group));
+            const int64_t at = int64_t(rq.first + tok) * a.q_heads + h * G + (i - tok * G);
+            part_ml[2 * at] = -INFINITY;
+            part_ml[2 * at + 1] = 0.0f;
+        }
+        return;
+    }
+
+    // places of the chunk's slots
+    for (int v = v0 + tid; v < v0 + a.chunk && v < v1 + kTile; v += kWg) {
+        const int j = rg.slot(v);
+        const int64_t row = v < v1 && j < rq.total ? slot_row(a.c, r, j) : -1;
+        s_off[v - v0] = row < 0 ? -1 : (row + h) * a.c.row_bytes;
+        s_pos[v - v0] = a.b.positions && j >= rq.ctx && j < rq.total ? a.b.positions[rq.first + j - rq.ctx] : j;
+        if constexpr (k8) {
+            s_ks[v - v0] = row < 0 ? 0.0f : a.c.scales[row + h];
+            s_vs[v - v0] = row < 0 ? 0.0f : a.c.scales[a.c.plane_scales + row + h];
+        }
+    }
+
+    // queries: rows n16 of each tile of 16, in the element order of K's pieces
+    u32x4 q[RT][DP / 32];
+    int tok[RT], qpos[RT];
+    float slope2[RT];
+    bool live[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = rt * 16 + n16;
+        live[rt] = row < rows;
+        const int rr = live[rt] ? row : 0;
+        tok[rt] = int(fast_div(uint32_t(rr), a.div_group));
+        const int head = h * G + (rr - tok[rt] * G);
+        qpos[rt] = a.b.positions ? a.b.positions[rq.first + tok[rt]] : rq.ctx + tok[rt];
+        slope2[rt] = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+        const uint16_t* src = a.q + int64_t(rq.first + tok[rt]) * a.q_stride + int64_t(head) * D;
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+            const int d = k8 ? (c >> 1) * 64 + g * 16 + (c & 1) * 8 : c * 32 + g * 8;
+            q[rt][c] = u32x4{0, 0, 0, 0};
+            if (live[rt] && d < D) q[rt][c] = *reinterpret_cast<const u32x4*>(src + d);
+        }
+    }
+    const ScoreArgs sc = score_args(a);
+    f32x4 o[RT][DT];
+    float m[RT], l[RT], ref = 0.0f;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[rt][t] = f32x4{0, 0, 0, 0};
+    }
+    __syncthreads();
+
+    const char* const kb = a.c.base;
+    const char* const vb = a.c.base + a.c.plane_bytes;
+
+    // Loads take no branch: a slot that lies in no page reads the plane's first
+    // row, a lane past the row's end its first piece.  What comes of the former is
+    // masked (turn), of the latter multiplied by q's zeros or not written.
+    int k_at[T::kPieces];
+#pragma unroll
+    for (int p = 0; p < T::kPieces; ++p) {
+        const int at = p * 64 + g * 16;
+        k_at[p] = at < a.c.row_bytes ? at : 0;
+    }
+    const int v_at = n16 * T::kVBytes < a.c.row_bytes ? n16 * T::kVBytes : 0;
+    const int v_more = v_at + 16 < a.c.row_bytes ? v_at + 16 : 0;   // the second piece of 32 bytes
+
+    auto load_k = [&](int v, T& x) {   // slot n16 of each half, 16-byte pieces g, g + 4, ...
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const char* const row = kb + max(s_off[v - v0 + 16 * s + n16], int64_t(0));
+#pragma unroll
+            for (int p = 0; p < T::kPieces; ++p) x.k[s][p] = load_words<16>(row + k_at[p]);
+        }
+    };
+    auto load_v = [&](int v, T& x) {   // slots 4 g .. 4 g + 3 of each half, elements n16 DT ..
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const char* const row = vb + max(s_off[v - v0 + 16 * (j >> 2) + 4 * g + (j & 3)], int64_t(0));
+            if constexpr (T::kVBytes == 32) {
+                const Words<16> y = load_words<16>(row + v_at), z = load_words<16>(row + v_more);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x.v[j].w[i] = y.w[i], x.v[j].w[4 + i] = z.w[i];
+            } else {
+                x.v[j] = load_words<T::kVBytes>(row + v_at);
+            }
+        }
+    };
+
+    // the t-th operand of O^T = V^T P^T
+    auto v_operand = [&](const T& x, int t) {
+        u32x4 f;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            if constexpr (!k8) {
+                const uint32_t a0 = x.v[2 * p].w[t >> 1], a1 = x.v[2 * p + 1].w[t >> 1];
+                f[p] = t & 1 ? pair16<true>(a0, a1) : pair16<false>(a0, a1);
+            } else {
+                const uint32_t a0 = x.v[2 * p].w[t >> 2], a1 = x.v[2 * p + 1].w[t >> 2];
+                const uint32_t y = __builtin_amdgcn_perm(a1, a0, t & 2 ? 0x07030602u : 0x05010400u);
+                f[p] = t & 1 ? widen2<kBf16, kCodes, true>(y) : widen2<kBf16, kCodes, false>(y);
+            }
+        }
+        return f;
+    };
+
+    auto turn = [&](int v, int next, T& x) {
+        const int j0 = rg.slot(v), at = v - v0;
+        // whether every row sees the tile whole
+        const uint64_t b0 = __ballot(s_off[at + n16] >= 0), b1 = __ballot(s_off[at + 16 + n16] >= 0);
+        const uint32_t valid = uint32_t(b0 & 0xFFFFu) | uint32_t(b1 & 0xFFFFu) << 16;
+        const bool whole = j0 >= rg.all_lo && j0 + kTile <= rg.all_hi && valid == ~0u;
+        float ks[2][4], vs[2][4];
+        if constexpr (k8) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    ks[s][i] = s_ks[at + 16 * s + 4 * g + i];
+                    vs[s][i] = s_vs[at + 16 * s + 4 * g + i];
+                }
+        }
+        float fresh_ref = 0.0f;
+        if constexpr (kRef) {
+            // the scales' largest, as a power of two that is not below it
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float y = __builtin_fabsf(vs[s][i]);
+                    fresh_ref = fmaxf(fresh_ref, y < INFINITY ? y : 0.0f);
+                }
+            fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 16));
+            fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 32));
+            const uint32_t e = (__float_as_uint(fresh_ref) + 0x7FFFFFu) & 0x7F800000u;
+            fresh_ref = __uint_as_float(min(max(e, 0x00800000u), 0x7E800000u));
+        }
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][e] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < DP / 32; ++c) {
+                u32x4 f;
+                if constexpr (k8) {
+                    const Words<16>& w = x.k[e][c >> 1];
+                    f = widen8<kBf16, kCodes>(w.w[2 * (c & 1)], w.w[2 * (c & 1) + 1]);
+                } else {
+                    const Words<16>& w = x.k[e][c];
+                    f = u32x4{w.w[0], w.w[1], w.w[2], w.w[3]};
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) s[rt][e] = mfma16<kBf16>(f, q[rt][c], s[rt][e]);
+            }
+        }
+        load_k(next, x);               // the next turn's keys take their place
+        u32x4 pf[RT], seen[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float y[2][4], top = -INFINITY;
+            if (!sc.general) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        y[e][i] = k8 ? s[rt][e][i] * (ks[e][i] * sc.c2) : s[rt][e][i] * sc.c2;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        y[e][i] = general_score(sc, k8 ? s[rt][e][i] * ks[e][i] : s[rt][e][i], slope2[rt],
+                                                qpos[rt] - s_pos[at + 16 * e + 4 * g + i]);
+            }
+            uint32_t mine = ~0u;
+            if (!whole) {
+                if (live[rt])
+                    mine = uint32_t(seen_of(a, rq, r, tok[rt], qpos[rt], j0, s_pos + at, valid));
+                mine >>= 4 * g;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(mine >> (16 * e + i) & 1u)) y[e][i] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, y[e][i]);
+            const bool grow = kRef && fresh_ref > ref;
+            if (__any(top > m[rt] + kSlack) || grow) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float to = fmaxf(m[rt], top);
+                float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - to);
+                l[rt] *= alpha;
+                m[rt] = to;
+                if (grow) alpha *= ref / fresh_ref;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[rt][t] *= alpha;
+            }
+            const float base = (m[rt] == -INFINITY ? 0.0f : m[rt]) - kShift<kBf16>;
+            const float per_ref = kRef ? 1.0f / fmaxf(ref, fresh_ref) : 1.0f;
+            float p[2][4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[e][i] = __builtin_amdgcn_exp2f(y[e][i] - base);
+                    l[rt] += p[e][i];
+                    if constexpr (kRef) p[e][i] *= vs[e][i] * per_ref;
+                    else if constexpr (k8) p[e][i] *= vs[e][i];
+                }
+            if (!whole) {
+                // a scale of a slot that is not seen may be anything
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool on = mine >> (16 * e + i) & 1u;
+                        if (k8 && !on) p[e][i] = 0.0f;
+                        const uint32_t one = on ? kOne<kBf16> : 0u;
+                        seen[rt][2 * e + (i >> 1)] = i & 1 ? seen[rt][2 * e + (i >> 1)] | one << 16 : one;
+                    }
+            }
+            pf[rt] = u32x4{pack2<kBf16>(p[0][0], p[0][1]), pack2<kBf16>(p[0][2], p[0][3]),
+                           pack2<kBf16>(p[1][0], p[1][1]), pack2<kBf16>(p[1][2], p[1][3])};
+        }
+        if constexpr (kRef) ref = fmaxf(ref, fresh_ref);
+        bool special = false;
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (!(valid >> (4 * g) >> (16 * (j >> 2) + (j & 3)) & 1u)) x.v[j] = no_words<T::kVBytes>();
+            uint32_t found = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < T::kVBytes / 4; ++i) found |= nonfinite<kBf16, kCodes>(x.v[j].w[i]);
+            special = __any(found != 0);
+        }
+        if (!special) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                const u32x4 f = v_operand(x, t);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma16<kBf16>(f, pf[rt], o[rt][t]);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                const u32x4 f = v_operand(x, t);
+                const f32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    o[rt][t] = mfma16<kBf16>(classify8<kBf16>(f, 0), pf[rt], o[rt][t]);
+                    const f32x4 up = mfma16<kBf16>(classify8<kBf16>(f, 1), seen[rt], zero);
+                    const f32x4 down = mfma16<kBf16>(classify8<kBf16>(f, 2), seen[rt], zero);
+                    const f32x4 nan = mfma16<kBf16>(classify8<kBf16>(f, 3), seen[rt], zero);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        o[rt][t][i] = with_specials(o[rt][t][i], up[i], down[i], nan[i]);
+                }
+                __builtin_amdgcn_sched_barrier(0);     // one at a time: this path is rare
+            }
+        }
+    };
+
+    int v = v0 + wave * kTile;
+    if (v < v1) {
+        T x;
+        load_k(v, x);
+        for (; v < v1; v += kWaves * kTile) {
+            load_v(v, x);
+            turn(v, v + kWaves * kTile < v1 ? v + kWaves * kTile : v, x);
+        }
+    }
+
+    // the waves' sums, joined through LDS two at a time
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 16);
+        l[rt] += __shfl_xor(l[rt], 32);
+        if (g == 0) {
+            s_ml[wave][rt * 16 + n16][0] = m[rt];
+            s_ml[wave][rt * 16 + n16][1] = l[rt];
+        }
+    }
+    __syncthreads();
+    float* const slab = reinterpret_cast<float*>(smem) + (wave & 1) * kRows * DP;
+    float scale[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_ml[w][rt * 16 + n16][0]);
+        scale[rt] = m[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[rt] - top);
+        if constexpr (kRef) scale[rt] *= ref;
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if ((wave >> 1) == half) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        float* const at = slab + (rt * 16 + n16) * DP + (4 * g + i) * DT + t;
+                        const float x = scale[rt] == 0.0f ? 0.0f : o[rt][t][i] * scale[rt];
+                        *at = half == 0 ? x : *at + x;
+                    }
+        }
+        __syncthreads();
+    }
+    const float* const sum = reinterpret_cast<const float*>(smem);
+    for (int i = tid; i < rows * (DP / 8); i += kWg) {
+        const int row = i / (DP / 8), d = i % (DP / 8) * 8;
+        if (d >= D) continue;
+        float top = -INFINITY, total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_ml[w][row][0]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            total += s_ml[w][row][0] == -INFINITY ? 0.0f
+                                                  : s_ml[w][row][1] * __builtin_amdgcn_exp2f(s_ml[w][row][0] - top);
+        const int t = int(fast_div(uint32_t(row), a.div_group));
+        const int64_t token = rq.first + t, head = h * G + (row - t * G);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = sum[row * DP + d + e] + sum[kRows * DP + row * DP + d + e];
+        if (a.splits > 1) {
+            const int64_t at = token * a.q_heads + head;
+            float4* const out = reinterpret_cast<float4*>(
+                a.part_o + (int64_t(split) * a.b.total_tokens * a.q_heads + at) * D + d);
+            out[0] = make_float4(x[0], x[1], x[2], x[3]);
+            out[1] = make_float4(x[4], x[5], x[6], x[7]);
+            if (d == 0) {
+                part_ml[2 * at] = top;
+                part_ml[2 * at + 1] = total;
+            }
+        } else {
+            const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = total == 0.0f ? 0u : pack2<kBf16>(x[2 * e] * inv, x[2 * e + 1] * inv);
+            *reinterpret_cast<u32x4*>(a.out + token * a.out_stride + head * D + d) = w;
+            if (a.lse && d == 0)
+                a.lse[token * a.q_heads + head] =
+                    total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total) - kShift<kBf16>) * kLn2;
+        }
+    }
+}
+
+template <bool kBf16, int kCodes, int DP, int RT>
+int go(const AttendArgs& a, void* stream)
+{
+    kvx_attend_few_kernel<kBf16, kCodes, DP, RT>
+        <<<dim3(uint32_t(a.c.num_requests) * a.splits * a.c.hd), dim3(kWg), 0,
+           static_cast<hipStream_t>(stream)>>>(a);
+    return int(hipGetLastError());
+}
+
+template <bool kBf16, int kCodes>
+int pick(const AttendArgs& a, const AttendPlan& p, void* stream)
+{
+    const bool two = p.tile_rows > 16;
+    if (a.c.dim <= 64) return two ? go<kBf16, kCodes, 64, 2>(a, stream) : go<kBf16, kCodes, 64, 1>(a, stream);
+    if (a.c.dim <= 128) return two ? go<kBf16, kCodes, 128, 2>(a, stream) : go<kBf16, kCodes, 128, 1>(a, stream);
+    return two ? go<kBf16, kCodes, 256, 2>(a, stream) : go<kBf16, kCodes, 256, 1>(a, stream);
+}
+
+}  // namespace
+
+int launch_few(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream)
+{
+    const bool bf = dtype == KVX_BF16;
+    switch (cache_dtype) {
+    case KVX_FP8_E4M3FN: return bf ? pick<true, kCodesE4m3>(a, p, stream) : pick<false, kCodesE4m3>(a, p, stream);
+    case KVX_FP8_E5M2: return bf ? pick<true, kCodesE5m2>(a, p, stream) : pick<false, kCodesE5m2>(a, p, stream);
+    default: return bf ? pick<true, kCodes16>(a, p, stream) : pick<false, kCodes16>(a, p, stream);
+    }
+}
+
+}  // namespace kvx

@@ -20,6 +20,9 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 // workgroups of one launch stay below 2^31
 constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
 
+// slots of one request
+constexpr int32_t kMaxSlots = 1 << 30;
+
 int64_t row_slots(const kvx_cache& c) { return int64_t(c.bt_stride) * c.block_size; }
 
 kvx_status check_shape(const kvx_cache* c)
@@ -71,6 +74,8 @@ kvx_status check_batch(const kvx_cache& c, const kvx_batch* b)
     if (b->max_context < 1 || b->max_context > row_slots(c))
         return fail(KVX_EINVAL, "max_context %d outside [1, %lld], the slots of a block-table row",
                     b->max_context, (long long)row_slots(c));
+    if (b->max_context > kMaxSlots)
+        return fail(KVX_EUNSUPPORTED, "max_context %d above 2^30", b->max_context);
     if (!b->token_starts || !b->contexts) return fail(KVX_EINVAL, "NULL token_starts or contexts");
     if (b->tree && (b->tree_stride < 1 || int64_t(b->tree_stride) * 64 < b->max_tokens))
         return fail(KVX_EINVAL, "tree_stride %d: %d tokens need a bit each", b->tree_stride,
@@ -104,7 +109,7 @@ kvx::CacheArgs cache_args(const kvx_cache& c, int layer0)
     a.block_size = c.block_size;
     a.hd = c.num_kv_heads;
     a.dim = c.head_dim;
-    a.row_slots = int32_t(std::min<int64_t>(row_slots(c), INT32_MAX));
+    a.row_slots = int32_t(std::min<int64_t>(row_slots(c), kMaxSlots));
     a.num_requests = c.num_requests;
     a.div_bs = kvx::make_fastdiv(uint32_t(c.block_size));
     return a;
@@ -181,6 +186,7 @@ kvx::AttendArgs attend_args(const kvx_cache& c, const kvx_batch& b, const kvx_sc
     a.window = s.window;
     a.q_heads = q_heads;
     a.group = q_heads / c.num_kv_heads;
+    a.div_group = kvx::make_fastdiv(uint32_t(a.group));
     return a;
 }
 
@@ -283,7 +289,8 @@ extern "C" kvx_status kvx_attend(const kvx_cache* c, const kvx_batch* b, const k
     a.lse = lse;
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    return launched(kvx::launch_attend(a, dtype, c->dtype, workspace, stream));
+    return launched(kvx::launch_attend(a, kvx::attend_plan(*c, *b, q_heads), dtype,
+                                       c->dtype, workspace, stream));
 }
 
 extern "C" kvx_status kvx_weigh(const kvx_cache* c, const kvx_batch* b, const kvx_scores* s,
@@ -321,6 +328,7 @@ extern "C" kvx_status kvx_evict(const kvx_cache* c, int32_t layer0, int32_t num_
     if (max_len < 0 || max_len > row_slots(*c))
         return fail(KVX_EINVAL, "max_len %d outside [0, %lld], the slots of a block-table row", max_len,
                     (long long)row_slots(*c));
+    if (max_len > kMaxSlots) return fail(KVX_EUNSUPPORTED, "max_len %d above 2^30", max_len);
     if (budget < 1 || sink < 0 || recent < 0 || int64_t(sink) + recent > budget)
         return fail(KVX_EINVAL, "budget %d must be >= 1 and hold sink %d + recent %d", budget, sink, recent);
     if (w_stride < max_len)

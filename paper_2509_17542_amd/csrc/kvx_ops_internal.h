@@ -107,13 +107,33 @@ struct AttendArgs {
     int32_t window;
     int32_t q_heads;
     int32_t group;
+    FastDiv div_group;
+    // a request's slots are dealt to `splits` workgroups, `chunk` slots each; more than one
+    // leave their sums here for kvx_join_kernel: part_o [split][N][q_heads][dim] and
+    // part_ml [split][N][q_heads] pairs (reference, sum of weights)
+    int32_t chunk, splits;
+    float* part_o;
+    float* part_ml;
 };
+
+// How a call is cut into workgroups.
+struct AttendPlan {
+    int rows;            // query rows of a KV head, at most
+    bool few;            // kvx_attend_few_kernel, else kvx_attend_rows_kernel
+    int row_tiles;       // workgroups along the rows (1 for few)
+    int tile_rows;       // rows of a workgroup
+    int chunk, splits;
+};
+AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
+int launch_few(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream);
+int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream);
 
 // Each enqueues its kernels on `stream` and returns a hipError_t value.
 int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream);
 int launch_evict(const EvictArgs& a, int num_layers, void* stream);
 int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void* stream);
-int launch_attend(const AttendArgs& a, int dtype, int cache_dtype, void* workspace, void* stream);
+int launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype,
+                  void* workspace, void* stream);
 int launch_weigh(const AttendArgs& a, int dtype, int cache_dtype, void* stream);
 uint64_t attend_workspace(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
 

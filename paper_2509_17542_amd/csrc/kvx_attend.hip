@@ -48,73 +48,6 @@ __device__ __forceinline__ float score(const AttendArgs& a, float dot, int head,
     return x;
 }
 
-// One wave per (token, query head): 64 slots at a time, a lane to each.
-template <bool kBf16, int kCache>
-__global__ void __launch_bounds__(64) kvx_attend_kernel(const AttendArgs a)
-{
-    __shared__ float qs[256], ps[64];
-    const int t = int(blockIdx.x) / a.q_heads, head = int(blockIdx.x) % a.q_heads;
-    const int lane = threadIdx.x, D = a.c.dim;
-    const int g = head / a.group;
-    uint16_t* out = a.out + t * a.out_stride + int64_t(head) * D;
-    const int r = request_at(a.b.starts, a.c.num_requests, t);
-    Request rq = {};
-    int i = 0;
-    if (r >= 0 && r < a.c.num_requests) {
-        rq = request_of(a.c, a.b, r);
-        i = t - rq.first;
-    }
-    for (int d = lane; d < D; d += 64)
-        qs[d] = value16<kBf16>(a.q[t * a.q_stride + int64_t(head) * D + d]);
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, o[4] = {};
-    const char* kb = a.c.base;
-    const char* vb = a.c.base + a.c.plane_bytes;
-    for (int j0 = 0; j0 < rq.total; j0 += 64) {
-        const int j = j0 + lane;
-        float x = -INFINITY, vs = 0.0f;
-        int64_t row = -1;
-        int dist;
-        if (j < rq.total && i < rq.n && visible(a, rq, r, i, j, dist)) row = slot_row(a.c, r, j);
-        if (row >= 0) {
-            const char* k = kb + (row + g) * a.c.row_bytes;
-            float dot = 0.0f;
-            for (int d = 0; d < D; ++d) dot = __builtin_fmaf(qs[d], element<kCache>(k, d), dot);
-            if constexpr (is8<kCache>()) {
-                dot *= a.c.scales[row + g];
-                vs = a.c.scales[a.c.plane_scales + row + g];
-            }
-            x = score(a, dot, head, dist);
-        }
-        float mt = x;
-        for (int s = 32; s; s >>= 1) mt = fmaxf(mt, __shfl_xor(mt, s));
-        const float mn = fmaxf(m, mt);
-        const float alpha = mn == -INFINITY ? 1.0f : __expf(m - mn);
-        const float p = x == -INFINITY ? 0.0f : __expf(x - mn);
-        float sum = p;
-        for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
-        l = l * alpha + sum;
-        m = mn;
-        for (int k = 0; k < 4; ++k) o[k] *= alpha;
-        __syncthreads();
-        ps[lane] = is8<kCache>() ? p * vs : p;
-        __syncthreads();
-        for (int jj = 0; jj < 64; ++jj) {
-            const int64_t rj = __shfl(row, jj);
-            if (rj < 0) continue;
-            const char* v = vb + (rj + g) * a.c.row_bytes;
-            for (int k = 0; k < 4; ++k)
-                if (lane + 64 * k < D)
-                    o[k] = __builtin_fmaf(ps[jj], element<kCache>(v, lane + 64 * k), o[k]);
-        }
-    }
-    for (int k = 0; k < 4; ++k)
-        if (lane + 64 * k < D)
-            out[lane + 64 * k] = uint16_t(bits16<kBf16>(l > 0.0f ? o[k] / l : 0.0f));
-    if (a.lse && lane == 0)
-        a.lse[int64_t(t) * a.q_heads + head] = l > 0.0f ? m + logf(l) : -INFINITY;
-}
-
 // One wave per (request, KV head, 64 slots): a lane to each slot.
 template <bool kBf16, int kCache>
 __global__ void __launch_bounds__(64) kvx_weigh_kernel(const AttendArgs a, int tiles)
@@ -215,14 +148,6 @@ int join(const AttendArgs& a, bool bf, void* stream)
 }
 
 template <bool kBf16, int kCache>
-int attend_as(const AttendArgs& a, void* stream)
-{
-    kvx_attend_kernel<kBf16, kCache><<<dim3(uint32_t(a.b.total_tokens) * a.q_heads), dim3(64), 0,
-                                       static_cast<hipStream_t>(stream)>>>(a);
-    return int(hipGetLastError());
-}
-
-template <bool kBf16, int kCache>
 int weigh_as(const AttendArgs& a, void* stream)
 {
     const int tiles = (a.b.max_context + 63) / 64;
@@ -242,16 +167,9 @@ int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int c
     a.splits = p.splits;
     a.part_ml = static_cast<float*>(workspace);
     a.part_o = a.part_ml + 2 * plan_pairs(a, p);
-    if (p.few) {
-        const int err = launch_few(a, p, dtype, cache_dtype, stream);
-        return err || p.splits == 1 ? err : join(a, bf, stream);
-    }
-    switch (cache_dtype) {
-    case KVX_FP16: return attend_as<false, KVX_FP16>(a, stream);
-    case KVX_BF16: return attend_as<true, KVX_BF16>(a, stream);
-    case KVX_FP8_E4M3FN: return bf ? attend_as<true, KVX_FP8_E4M3FN>(a, stream) : attend_as<false, KVX_FP8_E4M3FN>(a, stream);
-    default: return bf ? attend_as<true, KVX_FP8_E5M2>(a, stream) : attend_as<false, KVX_FP8_E5M2>(a, stream);
-    }
+    const int err = p.few ? launch_few(a, p, dtype, cache_dtype, stream)
+                          : launch_rows(a, p, dtype, cache_dtype, stream);
+    return err || p.splits == 1 ? err : join(a, bf, stream);
 }
 
 int launch_weigh(const AttendArgs& a, int dtype, int cache_dtype, void* stream)
@@ -270,10 +188,15 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
     AttendPlan p = {};
     p.rows = int(std::min<int64_t>(int64_t(b.max_tokens) * (q_heads / c.num_kv_heads), INT32_MAX));
     p.few = p.rows <= 32;
-    p.row_tiles = 1;
-    p.tile_rows = p.rows <= 16 ? 16 : 32;
+    p.tile_rows = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
+    p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     p.chunk = 512;
-    p.splits = p.few ? (b.max_context + p.chunk - 1) / p.chunk : 1;
+    if (!p.few) {
+        const int64_t groups = int64_t(c.num_requests) * c.num_kv_heads * p.row_tiles;
+        const int64_t want = std::max<int64_t>(1, 1024 / groups);
+        p.chunk = std::max(512, int((b.max_context + want - 1) / want + 63) & ~63);
+    }
+    p.splits = (b.max_context + p.chunk - 1) / p.chunk;
     return p;
 }
 

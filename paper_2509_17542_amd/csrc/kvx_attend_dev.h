@@ -137,11 +137,10 @@ __device__ __forceinline__ u32x4 classify8(u32x4 v, int kind)
                  classify2<kBf16>(v.z, kind), classify2<kBf16>(v.w, kind)};
 }
 
-__device__ __forceinline__ float with_specials(float o, float up, float down, float nan)
+// a sum `o` that the product of kind `kind` says had such values among its terms
+__device__ __forceinline__ float with_special(float o, float count, int kind)
 {
-    if (up > 0.0f) o += INFINITY;
-    if (down > 0.0f) o -= INFINITY;
-    return nan > 0.0f ? NAN : o;
+    return count > 0.0f ? o + (kind == 1 ? INFINITY : kind == 2 ? -INFINITY : NAN) : o;
 }
 
 // ---- visibility ------------------------------------------------------------------

@@ -366,12 +366,12 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     o[rt][t] = mfma16<kBf16>(classify8<kBf16>(f, 0), pf[rt], o[rt][t]);
-                    const f32x4 up = mfma16<kBf16>(classify8<kBf16>(f, 1), seen[rt], zero);
-                    const f32x4 down = mfma16<kBf16>(classify8<kBf16>(f, 2), seen[rt], zero);
-                    const f32x4 nan = mfma16<kBf16>(classify8<kBf16>(f, 3), seen[rt], zero);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        o[rt][t][i] = with_specials(o[rt][t][i], up[i], down[i], nan[i]);
+                    for (int kind = 1; kind <= 3; ++kind) {
+                        const f32x4 y = mfma16<kBf16>(classify8<kBf16>(f, kind), seen[rt], zero);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[rt][t][i] = with_special(o[rt][t][i], y[i], kind);
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);     // one at a time: this path is rare
             }

@@ -1,0 +1,457 @@
+// Attention of many query rows per KV head (wide trees, chains) over the paged
+// cache.
+//
+// A workgroup takes 32 rows per wave (rows are tokens times the query heads of
+// a KV head, tokens outermost) of one request and KV head, and walks the
+// slots that they see, KT at a time through LDS: K as rows, V transposed, both
+// widened to the queries' type and padded so that 16 lanes' 16-byte reads meet
+// every bank once.  While one tile is used the next one's rows are on their
+// way to registers, and the places of the one after that are looked up.
+//   S^T = K Q^T: a lane holds, of its query row, slots 8 q + 4 h + (0..3) of each
+//   32 (h: which half of the wave);
+//   O^T = V^T P^T: the weights go on as they lie, 8 of a lane's as one operand;
+//   V is laid out in LDS in that order of slots.
+// Workgroups that read the same slots are dealt to one XCD, next to each other.
+#include <hip/hip_runtime.h>
+
+#include "kvx_attend_dev.h"
+
+namespace kvx {
+namespace {
+
+template <int kCodes, int DP, int NW>
+struct Shape {
+    static constexpr int kWg = 64 * NW;
+    static constexpr int KT = DP >= 256 ? 32 : 64;          // slots of a tile
+    static constexpr int kEl = kCodes == kCodes16 ? 2 : 1;
+    static constexpr int kKRow = DP * 2 + 16;               // LDS bytes of a slot's K
+    static constexpr int kVRow = KT * 2 + 16;               // LDS bytes of an element's V
+    static constexpr int kKUnits = KT * DP / 8;             // 8 elements of a slot
+    static constexpr int kVUnits = (KT / 8) * (DP / 4);     // 4 elements of 8 slots
+    static constexpr int kKPer = (kKUnits + kWg - 1) / kWg;
+    static constexpr int kVPer = (kVUnits + kWg - 1) / kWg;
+    static constexpr int kRing = 4;                         // tiles whose places are known
+};
+
+template <bool kBf16, int kCodes, int DP, int NW>
+__global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_kernel(const AttendArgs a, int row_tiles)
+{
+    using S = Shape<kCodes, DP, NW>;
+    constexpr int KT = S::KT, kWg = S::kWg, ST = KT / 32, DTB = DP / 32;
+    constexpr bool k8 = kCodes != kCodes16;
+    constexpr bool kRef = k8 && !kBf16;
+    constexpr uint64_t kAll = KT == 64 ? ~uint64_t(0) : (uint64_t(1) << (KT & 63)) - 1;
+    __shared__ __attribute__((aligned(16))) char s_k[2][KT * S::kKRow];
+    __shared__ __attribute__((aligned(16))) char s_v[2][DP * S::kVRow];
+    __shared__ int64_t s_off[S::kRing][KT];
+    __shared__ __attribute__((aligned(16))) int32_t s_pos[S::kRing][KT];
+    __shared__ __attribute__((aligned(16))) float s_ks[k8 ? S::kRing : 1][k8 ? KT : 1];
+    __shared__ __attribute__((aligned(16))) float s_vs[k8 ? S::kRing : 1][k8 ? KT : 1];
+    __shared__ uint64_t s_valid[S::kRing];
+    __shared__ int s_special[S::kRing];
+
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n32 = lane & 31, half = lane >> 5;
+    const int D = a.c.dim, G = a.group;
+
+    // groups of workgroups over the same slots: consecutive blocks of one XCD
+    const uint32_t in_xcd = blockIdx.x / kXcds;
+    const uint32_t group = in_xcd / uint32_t(row_tiles) * kXcds + blockIdx.x % kXcds;
+    const int rt = int(in_xcd % uint32_t(row_tiles));
+    if (group >= uint32_t(a.c.num_requests) * uint32_t(a.splits) * uint32_t(a.c.hd)) return;
+    uint32_t u = group;
+    const int h = int(u % uint32_t(a.c.hd));
+    u /= uint32_t(a.c.hd);
+    const int split = int(u % uint32_t(a.splits)), r = int(u / uint32_t(a.splits));
+    const Request rq = request_of(a.c, a.b, r);
+    const int rows = rq.n * G, row0 = rt * 32 * NW;
+    if (row0 >= rows) return;
+    const int i0 = int(fast_div(uint32_t(row0), a.div_group));
+    const int i1 = int(fast_div(uint32_t(min(row0 + 32 * NW, rows) - 1), a.div_group));
+    const Range rg = range_of(a, rq, r, i0, i1);
+    const int v0 = split * a.chunk, v1 = min(v0 + a.chunk, rg.len);
+    const int tiles = v1 > v0 ? (v1 - v0 + KT - 1) / KT : 0;
+
+    // this lane's query row
+    const int row = row0 + wave * 32 + n32;
+    const bool live = row < rows;
+    const int rr = live ? row : row0;
+    const int tok = int(fast_div(uint32_t(rr), a.div_group)), head = h * G + (rr - tok * G);
+    const int64_t token = rq.first + tok;
+    const int qpos = a.b.positions ? a.b.positions[token] : rq.ctx + tok;
+    const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+    u32x4 q[DP / 16];
+    {
+        const uint16_t* const src = a.q + token * a.q_stride + int64_t(head) * D;
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) {
+            const int d = c * 16 + half * 8;
+            q[c] = u32x4{0, 0, 0, 0};
+            if (live && d < D) q[c] = *reinterpret_cast<const u32x4*>(src + d);
+        }
+    }
+    const ScoreArgs sc = score_args(a);
+    f32x16 o[DTB];
+#pragma unroll
+    for (int t = 0; t < DTB; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+    float m = -INFINITY, l = 0.0f, ref = 0.0f;
+
+    const char* const kb = a.c.base;
+    const char* const vb = a.c.base + a.c.plane_bytes;
+
+    // ---- places: the first wave looks them up, a lane to each slot of a tile ----
+    const bool finder = wave == 0 && lane < KT;
+    int64_t f_row = -1;
+    float f_ks = 0.0f, f_vs = 0.0f;
+    auto look_up = [&](int t) {
+        const int v = v0 + t * KT + lane, j = rg.slot(v);
+        f_row = finder && v < v1 && j < rq.total ? slot_row(a.c, r, j) : -1;
+    };
+    auto note_places = [&](int t) {
+        const int at = t & (S::kRing - 1);
+        if (wave == 0) {
+            const uint64_t valid = __ballot(f_row >= 0);
+            if (lane == 0) s_valid[at] = valid, s_special[at] = 0;
+        }
+        if (finder) {
+            const int j = rg.slot(v0 + t * KT + lane);
+            s_off[at][lane] = f_row < 0 ? -1 : (f_row + h) * a.c.row_bytes;
+            s_pos[at][lane] = a.b.positions && j >= rq.ctx && j < rq.total ? a.b.positions[rq.first + j - rq.ctx] : j;
+            if constexpr (k8) {
+                f_ks = f_row < 0 ? 0.0f : a.c.scales[f_row + h];
+                f_vs = f_row < 0 ? 0.0f : a.c.scales[a.c.plane_scales + f_row + h];
+            }
+        }
+    };
+    auto note_scales = [&](int t) {
+        if constexpr (k8) {
+            if (finder) {
+                s_ks[t & (S::kRing - 1)][lane] = f_ks;
+                s_vs[t & (S::kRing - 1)][lane] = f_vs;
+            }
+        }
+    };
+
+    // ---- rows of a tile: memory -> registers -> LDS ----
+    u32x4 kr[S::kKPer];
+    uint2 vr[S::kVPer][8];
+    auto load = [&](int t) {
+        const int64_t* const off = s_off[t & (S::kRing - 1)];
+#pragma unroll
+        for (int i = 0; i < S::kKPer; ++i) {
+            const int unit = tid + i * kWg;
+            if (S::kKUnits % kWg && unit >= S::kKUnits) break;
+            const int key = unit / (DP / 8), at = unit % (DP / 8) * 8 * S::kEl;
+            const char* const p = kb + max(off[key], int64_t(0)) + (at < a.c.row_bytes ? at : 0);
+            if constexpr (k8) {
+                const uint2 w = *reinterpret_cast<const uint2*>(p);
+                kr[i].x = w.x, kr[i].y = w.y;
+            } else {
+                kr[i] = *reinterpret_cast<const u32x4*>(p);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < S::kVPer; ++i) {
+            const int unit = tid + i * kWg;
+            if (S::kVUnits % kWg && unit >= S::kVUnits) break;
+            const int kg = unit / (DP / 4), at = unit % (DP / 4) * 4 * S::kEl;
+            const int first = (kg >> 1) * 16 + (kg & 1) * 4;
+            const int past = at < a.c.row_bytes ? at : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const char* const p = vb + max(off[first + (e & 3) + (e >> 2) * 8], int64_t(0)) + past;
+                if constexpr (k8)
+                    vr[i][e].x = *reinterpret_cast<const uint32_t*>(p);
+                else
+                    vr[i][e] = *reinterpret_cast<const uint2*>(p);
+            }
+        }
+    };
+    auto whole_tile = [&](int t) {
+        const int j0 = rg.slot(v0 + t * KT);
+        return j0 >= rg.all_lo && j0 + KT <= rg.all_hi && s_valid[t & (S::kRing - 1)] == kAll;
+    };
+    auto store = [&](int t) {
+        char* const ks = s_k[t & 1];
+        char* const vs = s_v[t & 1];
+        const bool whole = whole_tile(t);
+        const uint64_t valid = s_valid[t & (S::kRing - 1)];
+#pragma unroll
+        for (int i = 0; i < S::kKPer; ++i) {
+            const int unit = tid + i * kWg;
+            if (S::kKUnits % kWg && unit >= S::kKUnits) break;
+            const int key = unit / (DP / 8), d = unit % (DP / 8) * 8;
+            u32x4 w = kr[i];
+            if constexpr (k8) w = widen8<kBf16, kCodes>(kr[i].x, kr[i].y);
+            *reinterpret_cast<u32x4*>(ks + key * S::kKRow + d * 2) = w;
+        }
+#pragma unroll
+        for (int i = 0; i < S::kVPer; ++i) {
+            const int unit = tid + i * kWg;
+            if (S::kVUnits % kWg && unit >= S::kVUnits) break;
+            const int kg = unit / (DP / 4), d = unit % (DP / 4) * 4;
+            if (!whole) {
+                const int first = (kg >> 1) * 16 + (kg & 1) * 4;
+                uint32_t found = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (!(valid >> (first + (e & 3) + (e >> 2) * 8) & 1)) vr[i][e] = make_uint2(0, 0);
+                    found |= nonfinite<kBf16, kCodes>(vr[i][e].x);
+                    if constexpr (!k8) found |= nonfinite<kBf16, kCodes>(vr[i][e].y);
+                }
+                if (found) s_special[t & (S::kRing - 1)] = 1;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                u32x4 w;
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const uint2 x0 = vr[i][2 * p], x1 = vr[i][2 * p + 1];
+                    if constexpr (k8) {
+                        const uint32_t y = __builtin_amdgcn_perm(x1.x, x0.x, e & 2 ? 0x07030602u : 0x05010400u);
+                        w[p] = e & 1 ? widen2<kBf16, kCodes, true>(y) : widen2<kBf16, kCodes, false>(y);
+                    } else {
+                        const uint32_t y0 = e & 2 ? x0.y : x0.x, y1 = e & 2 ? x1.y : x1.x;
+                        w[p] = e & 1 ? pair16<true>(y0, y1) : pair16<false>(y0, y1);
+                    }
+                }
+                *reinterpret_cast<u32x4*>(vs + (d + e) * S::kVRow + kg * 16) = w;
+            }
+        }
+    };
+
+    auto use = [&](int t) {
+        const int ring = t & (S::kRing - 1), j0 = rg.slot(v0 + t * KT);
+        const bool whole = whole_tile(t);
+        const char* const kl = s_k[t & 1] + n32 * S::kKRow + half * 16;
+        const char* const vl = s_v[t & 1] + n32 * S::kVRow + half * 16;
+        f32x16 s[ST];
+#pragma unroll
+        for (int e = 0; e < ST; ++e) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[e][i] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c)
+                s[e] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(kl + e * 32 * S::kKRow + c * 32), q[c], s[e]);
+        }
+        // scores; element i of s[e] is slot 32 e + 8 (i / 4) + 4 half + i % 4
+        float fresh_ref = 0.0f;
+#pragma unroll
+        for (int e = 0; e < ST; ++e)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int at = 32 * e + 8 * b + 4 * half;
+                f32x4 ks = {1, 1, 1, 1};
+                if constexpr (k8) ks = *reinterpret_cast<const f32x4*>(&s_ks[ring][at]);
+                if constexpr (kRef) {
+                    const f32x4 vs = *reinterpret_cast<const f32x4*>(&s_vs[ring][at]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float y = __builtin_fabsf(vs[i]);
+                        fresh_ref = fmaxf(fresh_ref, y < INFINITY ? y : 0.0f);
+                    }
+                }
+                if (!sc.general) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[e][4 * b + i] *= k8 ? ks[i] * sc.c2 : sc.c2;
+                } else {
+                    const int4 pos = *reinterpret_cast<const int4*>(&s_pos[ring][at]);
+                    const int p[4] = {pos.x, pos.y, pos.z, pos.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        s[e][4 * b + i] = general_score(sc, k8 ? s[e][4 * b + i] * ks[i] : s[e][4 * b + i],
+                                                        slope2, qpos - p[i]);
+                }
+            }
+        uint64_t mine = ~uint64_t(0);
+        if (!whole) {
+            if (live) mine = seen_of(a, rq, r, tok, qpos, j0, s_pos[ring], s_valid[ring]);
+            mine >>= 4 * half;
+#pragma unroll
+            for (int e = 0; e < ST; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!(mine >> (32 * e + 8 * (i >> 2) + (i & 3)) & 1)) s[e][i] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < ST; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[e][i]);
+        if constexpr (kRef) {
+            fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 32));
+            const uint32_t e = (__float_as_uint(fresh_ref) + 0x7FFFFFu) & 0x7F800000u;
+            fresh_ref = __uint_as_float(min(max(e, 0x00800000u), 0x7E800000u));
+        }
+        const bool grow = kRef && fresh_ref > ref;
+        if (__any(top > m + kSlack) || grow) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float to = fmaxf(m, top);
+            float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            l *= alpha;
+            m = to;
+            if (grow) alpha *= ref / fresh_ref;
+#pragma unroll
+            for (int t2 = 0; t2 < DTB; ++t2) o[t2] *= alpha;
+        }
+        if constexpr (kRef) ref = fmaxf(ref, fresh_ref);
+        const float base = (m == -INFINITY ? 0.0f : m) - kShift<kBf16>;
+        const float per_ref = kRef ? 1.0f / ref : 1.0f;
+        u32x4 pf[ST][2];
+#pragma unroll
+        for (int e = 0; e < ST; ++e)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                float p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(s[e][4 * b + i] - base);
+                    l += p[i];
+                }
+                if constexpr (k8) {
+                    const f32x4 vs = *reinterpret_cast<const f32x4*>(&s_vs[ring][32 * e + 8 * b + 4 * half]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] *= kRef ? vs[i] * per_ref : vs[i];
+                    if (!whole) {
+                        // a scale of a slot that is not seen may be anything
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!(mine >> (32 * e + 8 * b + i) & 1)) p[i] = 0.0f;
+                    }
+                }
+                pf[e][b >> 1][2 * (b & 1)] = pack2<kBf16>(p[0], p[1]);
+                pf[e][b >> 1][2 * (b & 1) + 1] = pack2<kBf16>(p[2], p[3]);
+            }
+        if (whole || !s_special[ring]) {
+#pragma unroll
+            for (int e = 0; e < ST; ++e)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int t2 = 0; t2 < DTB; ++t2)
+                        o[t2] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + b * 32),
+                                              pf[e][b], o[t2]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < ST; ++e)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    u32x4 seen;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t two = uint32_t(mine >> (32 * e + 16 * b + 8 * (w >> 1) + 2 * (w & 1))) & 3u;
+                        seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
+                    }
+#pragma unroll
+                    for (int t2 = 0; t2 < DTB; ++t2) {
+                        const u32x4 f = *reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + b * 32);
+                        f32x16 zero;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
+                        o[t2] = mfma32<kBf16>(classify8<kBf16>(f, 0), pf[e][b], o[t2]);
+#pragma unroll
+                        for (int kind = 1; kind <= 3; ++kind) {
+                            const f32x16 x = mfma32<kBf16>(classify8<kBf16>(f, kind), seen, zero);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                o[t2][i] = with_special(o[t2][i], x[i], kind);
+                            __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
+                        }
+                    }
+                }
+        }
+    };
+
+    if (tiles > 0) {
+        look_up(0);
+        note_places(0);
+        note_scales(0);
+        look_up(1);
+        note_places(1);
+        look_up(2);
+        __syncthreads();
+        load(0);
+        for (int t = 0; t < tiles; ++t) {
+            store(t);
+            note_scales(t + 1);
+            note_places(t + 2);
+            look_up(t + 3);
+            __syncthreads();
+            if (t + 1 < tiles) load(t + 1);
+            use(t);
+        }
+    }
+
+    l += __shfl_xor(l, 32);
+    if (!live) return;
+    const int64_t at = token * a.q_heads + head;
+    if (a.splits > 1) {
+        const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
+        if (half == 0) {
+            a.part_ml[2 * (split * pairs + at)] = l == 0.0f ? -INFINITY : m;
+            a.part_ml[2 * (split * pairs + at) + 1] = l;
+        }
+        if (l == 0.0f) return;
+        float* const out = a.part_o + (split * pairs + at) * D;
+#pragma unroll
+        for (int t = 0; t < DTB; ++t)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int d = 32 * t + 8 * b + 4 * half;
+                f32x4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = kRef ? o[t][4 * b + i] * ref : o[t][4 * b + i];
+                if (d < D) *reinterpret_cast<f32x4*>(out + d) = x;
+            }
+    } else {
+        const float inv = l == 0.0f ? 0.0f : (kRef ? ref : 1.0f) / l;
+        uint16_t* const out = a.out + token * a.out_stride + int64_t(head) * D;
+#pragma unroll
+        for (int t = 0; t < DTB; ++t)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int d = 32 * t + 8 * b + 4 * half;
+                const uint2 w = l == 0.0f ? make_uint2(0, 0)
+                                          : make_uint2(pack2<kBf16>(o[t][4 * b] * inv, o[t][4 * b + 1] * inv),
+                                                       pack2<kBf16>(o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv));
+                if (d < D) *reinterpret_cast<uint2*>(out + d) = w;
+            }
+        if (a.lse && half == 0)
+            a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kShift<kBf16>) * kLn2;
+    }
+}
+
+template <bool kBf16, int kCodes, int DP, int NW>
+int go(const AttendArgs& a, const AttendPlan& p, void* stream)
+{
+    const int64_t groups = int64_t(a.c.num_requests) * a.splits * a.c.hd;
+    kvx_attend_rows_kernel<kBf16, kCodes, DP, NW>
+        <<<dim3(uint32_t((groups + kXcds - 1) / kXcds * kXcds * p.row_tiles)), dim3(64 * NW), 0,
+           static_cast<hipStream_t>(stream)>>>(a, p.row_tiles);
+    return int(hipGetLastError());
+}
+
+template <bool kBf16, int kCodes>
+int pick(const AttendArgs& a, const AttendPlan& p, void* stream)
+{
+    const bool two = p.tile_rows == 64;
+    if (a.c.dim <= 64) return two ? go<kBf16, kCodes, 64, 2>(a, p, stream) : go<kBf16, kCodes, 64, 4>(a, p, stream);
+    if (a.c.dim <= 128) return two ? go<kBf16, kCodes, 128, 2>(a, p, stream) : go<kBf16, kCodes, 128, 4>(a, p, stream);
+    return two ? go<kBf16, kCodes, 256, 2>(a, p, stream) : go<kBf16, kCodes, 256, 4>(a, p, stream);
+}
+
+}  // namespace
+
+int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream)
+{
+    const bool bf = dtype == KVX_BF16;
+    switch (cache_dtype) {
+    case KVX_FP8_E4M3FN: return bf ? pick<true, kCodesE4m3>(a, p, stream) : pick<false, kCodesE4m3>(a, p, stream);
+    case KVX_FP8_E5M2: return bf ? pick<true, kCodesE5m2>(a, p, stream) : pick<false, kCodesE5m2>(a, p, stream);
+    default: return bf ? pick<true, kCodes16>(a, p, stream) : pick<false, kCodes16>(a, p, stream);
+    }
+}
+
+}  // namespace kvx

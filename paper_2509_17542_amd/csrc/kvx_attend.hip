@@ -1,5 +1,4 @@
-// gfx950 kernels of attention over the paged cache (kvx_attend) and of the
-// slots' accumulated weights (kvx_weigh).
+// kvx_attend: how a call is cut into workgroups, and the join of its splits.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -8,76 +7,6 @@
 
 namespace kvx {
 namespace {
-
-template <int kCache>
-constexpr bool is8() { return kCache == KVX_FP8_E4M3FN || kCache == KVX_FP8_E5M2; }
-
-template <int kCache>
-__device__ __forceinline__ float element(const char* row, int i)
-{
-    if constexpr (is8<kCache>())
-        return value8<kCache == KVX_FP8_E5M2, 0>(reinterpret_cast<const uint8_t*>(row)[i]);
-    else
-        return value16<kCache == KVX_BF16>(reinterpret_cast<const uint16_t*>(row)[i]);
-}
-
-// Whether token i of request r sees slot j, and the distance between them.
-__device__ __forceinline__ bool visible(const AttendArgs& a, const Request& rq, int r, int i, int j,
-                                        int& distance)
-{
-    const int tok = rq.first + i;
-    const int qp = a.b.positions ? a.b.positions[tok] : rq.ctx + i;
-    const int kp = j >= rq.ctx && a.b.positions ? a.b.positions[rq.first + j - rq.ctx] : j;
-    distance = qp - kp;
-    if (j >= rq.total) return false;
-    if (a.prefix && j < a.prefix[r]) return true;
-    bool see = true;
-    if (j >= rq.ctx) {
-        const int k = j - rq.ctx;
-        see = a.b.tree ? (a.b.tree[int64_t(tok) * a.b.tree_stride + (k >> 6)] >> (k & 63)) & 1
-                       : k <= i;
-    }
-    return see && (a.window <= 0 || distance < a.window);
-}
-
-__device__ __forceinline__ float score(const AttendArgs& a, float dot, int head, int distance)
-{
-    float x = dot * a.scale;
-    if (a.softcap > 0.0f) x = a.softcap * tanhf(x / a.softcap);
-    if (a.slopes) x -= a.slopes[head] * static_cast<float>(abs(distance));
-    return x;
-}
-
-// One wave per (request, KV head, 64 slots): a lane to each slot.
-template <bool kBf16, int kCache>
-__global__ void __launch_bounds__(64) kvx_weigh_kernel(const AttendArgs a, int tiles)
-{
-    const int lane = threadIdx.x, D = a.c.dim;
-    const int g = (int(blockIdx.x) / tiles) % a.c.hd, r = int(blockIdx.x) / tiles / a.c.hd;
-    const Request rq = request_of(a.c, a.b, r);
-    const int j = int(blockIdx.x) % tiles * 64 + lane;
-    if (j >= rq.total) return;
-    const int64_t row = slot_row(a.c, r, j);
-    float w = 0.0f;
-    if (row >= 0) {
-        const char* k = a.c.base + (row + g) * a.c.row_bytes;
-        for (int i = 0; i < rq.n; ++i) {
-            int dist;
-            if (!visible(a, rq, r, i, j, dist)) continue;
-            for (int h = g * a.group; h < (g + 1) * a.group; ++h) {
-                const uint16_t* q = a.q + int64_t(rq.first + i) * a.q_stride + int64_t(h) * D;
-                float dot = 0.0f;
-                for (int d = 0; d < D; ++d)
-                    dot = __builtin_fmaf(value16<kBf16>(q[d]), element<kCache>(k, d), dot);
-                if constexpr (is8<kCache>()) dot *= a.c.scales[row + g];
-                const float lse = a.lse[int64_t(rq.first + i) * a.q_heads + h];
-                if (lse > -INFINITY) w += __expf(score(a, dot, h, dist) - lse);
-            }
-        }
-    }
-    float* out = a.weights + (int64_t(r) * a.c.hd + g) * a.w_stride + j;
-    *out = j < rq.ctx ? *out + w : w;
-}
 
 // ---- splits joined -------------------------------------------------------------
 //
@@ -147,15 +76,6 @@ int join(const AttendArgs& a, bool bf, void* stream)
     return int(hipGetLastError());
 }
 
-template <bool kBf16, int kCache>
-int weigh_as(const AttendArgs& a, void* stream)
-{
-    const int tiles = (a.b.max_context + 63) / 64;
-    kvx_weigh_kernel<kBf16, kCache><<<dim3(uint32_t(tiles) * a.c.hd * a.c.num_requests), dim3(64), 0,
-                                      static_cast<hipStream_t>(stream)>>>(a, tiles);
-    return int(hipGetLastError());
-}
-
 }  // namespace
 
 int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int cache_dtype,
@@ -170,17 +90,6 @@ int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int c
     const int err = p.few ? launch_few(a, p, dtype, cache_dtype, stream)
                           : launch_rows(a, p, dtype, cache_dtype, stream);
     return err || p.splits == 1 ? err : join(a, bf, stream);
-}
-
-int launch_weigh(const AttendArgs& a, int dtype, int cache_dtype, void* stream)
-{
-    const bool bf = dtype == KVX_BF16;
-    switch (cache_dtype) {
-    case KVX_FP16: return weigh_as<false, KVX_FP16>(a, stream);
-    case KVX_BF16: return weigh_as<true, KVX_BF16>(a, stream);
-    case KVX_FP8_E4M3FN: return bf ? weigh_as<true, KVX_FP8_E4M3FN>(a, stream) : weigh_as<false, KVX_FP8_E4M3FN>(a, stream);
-    default: return bf ? weigh_as<true, KVX_FP8_E5M2>(a, stream) : weigh_as<false, KVX_FP8_E5M2>(a, stream);
-    }
 }
 
 AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)

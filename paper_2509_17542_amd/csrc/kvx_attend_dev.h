@@ -96,9 +96,10 @@ __device__ __forceinline__ uint32_t pair16(uint32_t key0, uint32_t key1)
 // ---- non-finite values ---------------------------------------------------------
 //
 // A weight of 0 does not hide an infinity from a matrix product (0 x inf is
-// NaN).  Where a tile is not seen whole by every row and its values are not all
-// finite, the product takes the finite ones, and three products of ones with
-// the rows' visibility say which sums had +inf, -inf or NaN among them.
+// NaN).  Where a tile is not seen whole by every row, the product takes its
+// finite values only; if there were others, a second walk over such tiles, after
+// the first, finds by three products of ones with the rows' visibility which
+// sums have +inf, -inf or NaN among their terms.
 
 template <bool kBf16>
 constexpr uint32_t kOne = kBf16 ? 0x3F80u : 0x3C00u;
@@ -113,6 +114,13 @@ __device__ __forceinline__ uint32_t nonfinite(uint32_t w)
     if constexpr (kCodes == kCodesE5m2) return ((w & 0x7C7C7C7Cu) + 0x04040404u) & 0x80808080u;
     return kBf16 ? ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u
                  : ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+}
+
+// a word with its elements or codes that are not finite as 0
+template <int kCodes>
+__device__ __forceinline__ uint32_t without(uint32_t w, uint32_t found)
+{
+    return w & ~(kCodes == kCodes16 ? (found >> 15) * 0xFFFFu : (found >> 7) * 0xFFu);
 }
 
 // kind 0: finite values kept, others 0; 1: one where +inf; 2: -inf; 3: NaN

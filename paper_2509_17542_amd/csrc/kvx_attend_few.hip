@@ -76,7 +76,7 @@ struct Tile {
 template <int DP, int RT>
 constexpr int kWavesPerSimd = DP >= 256 ? 1 : DP * RT >= 128 ? 2 : 3;
 
-template <bool kBf16, int kCodes, int DP, int RT>
+template <bool kBf16, int kCodes, int DP, int RT, bool kGeneral>
 __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_kernel(const AttendArgs a)
 {
     using T = Tile<kCodes, DP>;
@@ -215,12 +215,33 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
         return f;
     };
 
+    // the tile's slots that lie in a page
+    auto valid_of = [&](int v) {
+        const uint64_t b0 = __ballot(s_off[v - v0 + n16] >= 0), b1 = __ballot(s_off[v - v0 + 16 + n16] >= 0);
+        return uint32_t(b0 & 0xFFFFu) | uint32_t(b1 & 0xFFFFu) << 16;
+    };
+    // whether every row sees the tile whole
+    auto is_whole = [&](int v, uint32_t valid) {
+        const int j0 = rg.slot(v);
+        return j0 >= rg.all_lo && j0 + kTile <= rg.all_hi && valid == ~0u;
+    };
+    // what row tile rt sees of it, bit 16 e + i: slot 16 e + 4 g + i
+    auto seen_by = [&](int rt, int v, uint32_t valid) {
+        const uint64_t m = live[rt] ? seen_of(a, rq, r, tok[rt], qpos[rt], rg.slot(v), s_pos + v - v0, valid) : 0;
+        return uint32_t(m) >> (4 * g);
+    };
+    // V's slots that lie in no page were read from another
+    auto drop_v = [&](T& x, uint32_t valid) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!(valid >> (4 * g) >> (16 * (j >> 2) + (j & 3)) & 1u)) x.v[j] = no_words<T::kVBytes>();
+    };
+    bool special = false;
+
     auto turn = [&](int v, int next, T& x) {
-        const int j0 = rg.slot(v), at = v - v0;
-        // whether every row sees the tile whole
-        const uint64_t b0 = __ballot(s_off[at + n16] >= 0), b1 = __ballot(s_off[at + 16 + n16] >= 0);
-        const uint32_t valid = uint32_t(b0 & 0xFFFFu) | uint32_t(b1 & 0xFFFFu) << 16;
-        const bool whole = j0 >= rg.all_lo && j0 + kTile <= rg.all_hi && valid == ~0u;
+        const int at = v - v0;
+        const uint32_t valid = valid_of(v);
+        const bool whole = is_whole(v, valid);
         float ks[2][4], vs[2][4];
         if constexpr (k8) {
 #pragma unroll
@@ -266,11 +287,11 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
             }
         }
         load_k(next, x);               // the next turn's keys take their place
-        u32x4 pf[RT], seen[RT];
+        u32x4 pf[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             float y[2][4], top = -INFINITY;
-            if (!sc.general) {
+            if constexpr (!kGeneral) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -286,9 +307,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
             }
             uint32_t mine = ~0u;
             if (!whole) {
-                if (live[rt])
-                    mine = uint32_t(seen_of(a, rq, r, tok[rt], qpos[rt], j0, s_pos + at, valid));
-                mine >>= 4 * g;
+                mine = seen_by(rt, v, valid);
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -323,58 +342,36 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
                     if constexpr (kRef) p[e][i] *= vs[e][i] * per_ref;
                     else if constexpr (k8) p[e][i] *= vs[e][i];
                 }
-            if (!whole) {
+            if (k8 && !whole) {
                 // a scale of a slot that is not seen may be anything
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bool on = mine >> (16 * e + i) & 1u;
-                        if (k8 && !on) p[e][i] = 0.0f;
-                        const uint32_t one = on ? kOne<kBf16> : 0u;
-                        seen[rt][2 * e + (i >> 1)] = i & 1 ? seen[rt][2 * e + (i >> 1)] | one << 16 : one;
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        if (!(mine >> (16 * e + i) & 1u)) p[e][i] = 0.0f;
             }
             pf[rt] = u32x4{pack2<kBf16>(p[0][0], p[0][1]), pack2<kBf16>(p[0][2], p[0][3]),
                            pack2<kBf16>(p[1][0], p[1][1]), pack2<kBf16>(p[1][2], p[1][3])};
         }
         if constexpr (kRef) ref = fmaxf(ref, fresh_ref);
-        bool special = false;
         if (!whole) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (!(valid >> (4 * g) >> (16 * (j >> 2) + (j & 3)) & 1u)) x.v[j] = no_words<T::kVBytes>();
+            drop_v(x, valid);
             uint32_t found = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int i = 0; i < T::kVBytes / 4; ++i) found |= nonfinite<kBf16, kCodes>(x.v[j].w[i]);
-            special = __any(found != 0);
-        }
-        if (!special) {
-#pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                const u32x4 f = v_operand(x, t);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma16<kBf16>(f, pf[rt], o[rt][t]);
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                const u32x4 f = v_operand(x, t);
-                const f32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    o[rt][t] = mfma16<kBf16>(classify8<kBf16>(f, 0), pf[rt], o[rt][t]);
-#pragma unroll
-                    for (int kind = 1; kind <= 3; ++kind) {
-                        const f32x4 y = mfma16<kBf16>(classify8<kBf16>(f, kind), seen[rt], zero);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[rt][t][i] = with_special(o[rt][t][i], y[i], kind);
-                    }
+                for (int i = 0; i < T::kVBytes / 4; ++i) {
+                    const uint32_t f = nonfinite<kBf16, kCodes>(x.v[j].w[i]);
+                    x.v[j].w[i] = without<kCodes>(x.v[j].w[i], f);
+                    found |= f;
                 }
-                __builtin_amdgcn_sched_barrier(0);     // one at a time: this path is rare
-            }
+            special |= __any(found != 0) != 0;
+        }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            const u32x4 f = v_operand(x, t);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma16<kBf16>(f, pf[rt], o[rt][t]);
         }
     };
 
@@ -385,6 +382,37 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
         for (; v < v1; v += kWaves * kTile) {
             load_v(v, x);
             turn(v, v + kWaves * kTile < v1 ? v + kWaves * kTile : v, x);
+        }
+    }
+    if (__builtin_expect(special, 0)) {
+        // the tiles that not every row sees whole again: which sums had infinities or NaN
+        for (v = v0 + wave * kTile; v < v1; v += kWaves * kTile) {
+            const uint32_t valid = valid_of(v);
+            if (is_whole(v, valid)) continue;
+            T x;
+            load_v(v, x);
+            drop_v(x, valid);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const uint32_t mine = seen_by(rt, v, valid);
+                u32x4 seen;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t two = mine >> (16 * (w >> 1) + 2 * (w & 1)) & 3u;
+                    seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
+                }
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    const u32x4 f = v_operand(x, t);
+#pragma unroll
+                    for (int kind = 1; kind <= 3; ++kind) {
+                        const f32x4 count = mfma16<kBf16>(classify8<kBf16>(f, kind), seen, f32x4{0, 0, 0, 0});
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[rt][t][i] = with_special(o[rt][t][i], count[i], kind);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
+                }
+            }
         }
     }
 
@@ -465,13 +493,20 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
     }
 }
 
-template <bool kBf16, int kCodes, int DP, int RT>
-int go(const AttendArgs& a, void* stream)
+template <bool kBf16, int kCodes, int DP, int RT, bool kGeneral>
+int go_as(const AttendArgs& a, void* stream)
 {
-    kvx_attend_few_kernel<kBf16, kCodes, DP, RT>
+    kvx_attend_few_kernel<kBf16, kCodes, DP, RT, kGeneral>
         <<<dim3(uint32_t(a.c.num_requests) * a.splits * a.c.hd), dim3(kWg), 0,
            static_cast<hipStream_t>(stream)>>>(a);
     return int(hipGetLastError());
+}
+
+template <bool kBf16, int kCodes, int DP, int RT>
+int go(const AttendArgs& a, void* stream)
+{
+    return a.softcap > 0.0f || a.slopes ? go_as<kBf16, kCodes, DP, RT, true>(a, stream)
+                                        : go_as<kBf16, kCodes, DP, RT, false>(a, stream);
 }
 
 template <bool kBf16, int kCodes>

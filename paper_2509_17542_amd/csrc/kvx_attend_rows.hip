@@ -33,7 +33,7 @@ struct Shape {
     static constexpr int kRing = 4;                         // tiles whose places are known
 };
 
-template <bool kBf16, int kCodes, int DP, int NW>
+template <bool kBf16, int kCodes, int DP, int NW, bool kGeneral>
 __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_kernel(const AttendArgs a, int row_tiles)
 {
     using S = Shape<kCodes, DP, NW>;
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     __shared__ __attribute__((aligned(16))) float s_ks[k8 ? S::kRing : 1][k8 ? KT : 1];
     __shared__ __attribute__((aligned(16))) float s_vs[k8 ? S::kRing : 1][k8 ? KT : 1];
     __shared__ uint64_t s_valid[S::kRing];
-    __shared__ int s_special[S::kRing];
+    __shared__ int s_special;
 
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -101,6 +101,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     const char* const kb = a.c.base;
     const char* const vb = a.c.base + a.c.plane_bytes;
 
+    if (tid == 0) s_special = 0;
+
     // ---- places: the first wave looks them up, a lane to each slot of a tile ----
     const bool finder = wave == 0 && lane < KT;
     int64_t f_row = -1;
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         const int at = t & (S::kRing - 1);
         if (wave == 0) {
             const uint64_t valid = __ballot(f_row >= 0);
-            if (lane == 0) s_valid[at] = valid, s_special[at] = 0;
+            if (lane == 0) s_valid[at] = valid;
         }
         if (finder) {
             const int j = rg.slot(v0 + t * KT + lane);
@@ -173,7 +175,26 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         const int j0 = rg.slot(v0 + t * KT);
         return j0 >= rg.all_lo && j0 + KT <= rg.all_hi && s_valid[t & (S::kRing - 1)] == kAll;
     };
-    auto store = [&](int t) {
+    // element e of 8 slots, in the queries' type
+    auto column = [&](const uint2 (&x)[8], int e) {
+        u32x4 w;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            if constexpr (k8) {
+                const uint32_t y = __builtin_amdgcn_perm(x[2 * p + 1].x, x[2 * p].x,
+                                                         e & 2 ? 0x07030602u : 0x05010400u);
+                w[p] = e & 1 ? widen2<kBf16, kCodes, true>(y) : widen2<kBf16, kCodes, false>(y);
+            } else {
+                const uint32_t y0 = e & 2 ? x[2 * p].y : x[2 * p].x;
+                const uint32_t y1 = e & 2 ? x[2 * p + 1].y : x[2 * p + 1].x;
+                w[p] = e & 1 ? pair16<true>(y0, y1) : pair16<false>(y0, y1);
+            }
+        }
+        return w;
+    };
+    // kind 0: K, and V with its values that are not finite as 0 where not every row sees the
+    // tile whole; 1 to 3: ones where V is +inf, -inf, NaN
+    auto store = [&](int t, int kind) {
         char* const ks = s_k[t & 1];
         char* const vs = s_v[t & 1];
         const bool whole = whole_tile(t);
@@ -192,38 +213,40 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             const int unit = tid + i * kWg;
             if (S::kVUnits % kWg && unit >= S::kVUnits) break;
             const int kg = unit / (DP / 4), d = unit % (DP / 4) * 4;
+            uint32_t found = 0;
             if (!whole) {
                 const int first = (kg >> 1) * 16 + (kg & 1) * 4;
-                uint32_t found = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if (!(valid >> (first + (e & 3) + (e >> 2) * 8) & 1)) vr[i][e] = make_uint2(0, 0);
                     found |= nonfinite<kBf16, kCodes>(vr[i][e].x);
                     if constexpr (!k8) found |= nonfinite<kBf16, kCodes>(vr[i][e].y);
                 }
-                if (found) s_special[t & (S::kRing - 1)] = 1;
             }
+            if (__builtin_expect(kind > 0 || found, 0)) {
+                if (found && kind == 0) s_special = 1;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                u32x4 w;
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    const uint2 x0 = vr[i][2 * p], x1 = vr[i][2 * p + 1];
-                    if constexpr (k8) {
-                        const uint32_t y = __builtin_amdgcn_perm(x1.x, x0.x, e & 2 ? 0x07030602u : 0x05010400u);
-                        w[p] = e & 1 ? widen2<kBf16, kCodes, true>(y) : widen2<kBf16, kCodes, false>(y);
-                    } else {
-                        const uint32_t y0 = e & 2 ? x0.y : x0.x, y1 = e & 2 ? x1.y : x1.x;
-                        w[p] = e & 1 ? pair16<true>(y0, y1) : pair16<false>(y0, y1);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    *reinterpret_cast<u32x4*>(vs + (d + e) * S::kVRow + kg * 16) =
+                        classify8<kBf16>(column(vr[i], e), kind);
+                    __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
                 }
-                *reinterpret_cast<u32x4*>(vs + (d + e) * S::kVRow + kg * 16) = w;
+                continue;
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<u32x4*>(vs + (d + e) * S::kVRow + kg * 16) = column(vr[i], e);
         }
     };
 
+    auto seen_by_me = [&](int t) {
+        const int ring = t & (S::kRing - 1);
+        uint64_t mine = ~uint64_t(0);
+        if (live) mine = seen_of(a, rq, r, tok, qpos, rg.slot(v0 + t * KT), s_pos[ring], s_valid[ring]);
+        return mine >> (4 * half);
+    };
     auto use = [&](int t) {
-        const int ring = t & (S::kRing - 1), j0 = rg.slot(v0 + t * KT);
+        const int ring = t & (S::kRing - 1);
         const bool whole = whole_tile(t);
         const char* const kl = s_k[t & 1] + n32 * S::kKRow + half * 16;
         const char* const vl = s_v[t & 1] + n32 * S::kVRow + half * 16;
@@ -253,7 +276,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                         fresh_ref = fmaxf(fresh_ref, y < INFINITY ? y : 0.0f);
                     }
                 }
-                if (!sc.general) {
+                if constexpr (!kGeneral) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[e][4 * b + i] *= k8 ? ks[i] * sc.c2 : sc.c2;
                 } else {
@@ -267,8 +290,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             }
         uint64_t mine = ~uint64_t(0);
         if (!whole) {
-            if (live) mine = seen_of(a, rq, r, tok, qpos, j0, s_pos[ring], s_valid[ring]);
-            mine >>= 4 * half;
+            mine = seen_by_me(t);
 #pragma unroll
             for (int e = 0; e < ST; ++e)
 #pragma unroll
@@ -324,44 +346,14 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 pf[e][b >> 1][2 * (b & 1)] = pack2<kBf16>(p[0], p[1]);
                 pf[e][b >> 1][2 * (b & 1) + 1] = pack2<kBf16>(p[2], p[3]);
             }
-        if (whole || !s_special[ring]) {
 #pragma unroll
-            for (int e = 0; e < ST; ++e)
+        for (int e = 0; e < ST; ++e)
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int t2 = 0; t2 < DTB; ++t2)
-                        o[t2] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + b * 32),
-                                              pf[e][b], o[t2]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < ST; ++e)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    u32x4 seen;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint32_t two = uint32_t(mine >> (32 * e + 16 * b + 8 * (w >> 1) + 2 * (w & 1))) & 3u;
-                        seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
-                    }
-#pragma unroll
-                    for (int t2 = 0; t2 < DTB; ++t2) {
-                        const u32x4 f = *reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + b * 32);
-                        f32x16 zero;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
-                        o[t2] = mfma32<kBf16>(classify8<kBf16>(f, 0), pf[e][b], o[t2]);
-#pragma unroll
-                        for (int kind = 1; kind <= 3; ++kind) {
-                            const f32x16 x = mfma32<kBf16>(classify8<kBf16>(f, kind), seen, zero);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                o[t2][i] = with_special(o[t2][i], x[i], kind);
-                            __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
-                        }
-                    }
-                }
-        }
+                for (int t2 = 0; t2 < DTB; ++t2)
+                    o[t2] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + b * 32),
+                                          pf[e][b], o[t2]);
     };
 
     if (tiles > 0) {
@@ -374,13 +366,52 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         __syncthreads();
         load(0);
         for (int t = 0; t < tiles; ++t) {
-            store(t);
+            store(t, 0);
             note_scales(t + 1);
             note_places(t + 2);
             look_up(t + 3);
             __syncthreads();
             if (t + 1 < tiles) load(t + 1);
             use(t);
+        }
+        __syncthreads();
+        if (__builtin_expect(s_special, 0)) {
+            // the tiles that not every row sees whole again: which sums had infinities or NaN
+            for (int t = 0; t < tiles; ++t) {
+                __syncthreads();
+                look_up(t);
+                note_places(t);
+                __syncthreads();
+                if (whole_tile(t)) continue;
+                const uint64_t mine = live ? seen_by_me(t) : 0;
+                for (int kind = 1; kind <= 3; ++kind) {
+                    load(t);
+                    store(t, kind);
+                    __syncthreads();
+                    const char* const vl = s_v[t & 1] + n32 * S::kVRow + half * 16;
+#pragma unroll
+                    for (int t2 = 0; t2 < DTB; ++t2) {
+                        f32x16 count;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) count[i] = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 2 * ST; ++e) {
+                            u32x4 seen;
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                const uint32_t two = uint32_t(mine >> (16 * e + 8 * (w >> 1) + 2 * (w & 1))) & 3u;
+                                seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
+                            }
+                            count = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 32),
+                                                  seen, count);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[t2][i] = with_special(o[t2][i], count[i], kind);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    __syncthreads();
+                }
+            }
         }
     }
 
@@ -423,14 +454,21 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     }
 }
 
-template <bool kBf16, int kCodes, int DP, int NW>
-int go(const AttendArgs& a, const AttendPlan& p, void* stream)
+template <bool kBf16, int kCodes, int DP, int NW, bool kGeneral>
+int go_as(const AttendArgs& a, const AttendPlan& p, void* stream)
 {
     const int64_t groups = int64_t(a.c.num_requests) * a.splits * a.c.hd;
-    kvx_attend_rows_kernel<kBf16, kCodes, DP, NW>
+    kvx_attend_rows_kernel<kBf16, kCodes, DP, NW, kGeneral>
         <<<dim3(uint32_t((groups + kXcds - 1) / kXcds * kXcds * p.row_tiles)), dim3(64 * NW), 0,
            static_cast<hipStream_t>(stream)>>>(a, p.row_tiles);
     return int(hipGetLastError());
+}
+
+template <bool kBf16, int kCodes, int DP, int NW>
+int go(const AttendArgs& a, const AttendPlan& p, void* stream)
+{
+    return a.softcap > 0.0f || a.slopes ? go_as<kBf16, kCodes, DP, NW, true>(a, p, stream)
+                                        : go_as<kBf16, kCodes, DP, NW, false>(a, p, stream);
 }
 
 template <bool kBf16, int kCodes>

@@ -254,6 +254,13 @@ struct ScoreArgs {
     bool general;    // capped or biased
 };
 
+// Scores that are more than a product with a positive scale: the others' largest
+// is found before they are scaled.
+inline bool general_scores(const AttendArgs& a)
+{
+    return a.softcap > 0.0f || a.slopes || !(a.scale > 0.0f);
+}
+
 __device__ __forceinline__ ScoreArgs score_args(const AttendArgs& a)
 {
     ScoreArgs s;

@@ -505,7 +505,7 @@ int go_as(const AttendArgs& a, void* stream)
 template <bool kBf16, int kCodes, int DP, int RT>
 int go(const AttendArgs& a, void* stream)
 {
-    return a.softcap > 0.0f || a.slopes ? go_as<kBf16, kCodes, DP, RT, true>(a, stream)
+    return general_scores(a) ? go_as<kBf16, kCodes, DP, RT, true>(a, stream)
                                         : go_as<kBf16, kCodes, DP, RT, false>(a, stream);
 }
 

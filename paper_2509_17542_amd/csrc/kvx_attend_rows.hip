@@ -54,11 +54,10 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     const int n32 = lane & 31, half = lane >> 5;
     const int D = a.c.dim, G = a.group;
 
-    // groups of workgroups over the same slots: consecutive blocks of one XCD
-    const uint32_t in_xcd = blockIdx.x / kXcds;
-    const uint32_t group = in_xcd / uint32_t(row_tiles) * kXcds + blockIdx.x % kXcds;
-    const int rt = int(in_xcd % uint32_t(row_tiles));
-    if (group >= uint32_t(a.c.num_requests) * uint32_t(a.splits) * uint32_t(a.c.hd)) return;
+    // the last rows, which see the most slots, first
+    const uint32_t groups = uint32_t(a.c.num_requests) * uint32_t(a.splits) * uint32_t(a.c.hd);
+    const uint32_t group = blockIdx.x % groups;
+    const int rt = row_tiles - 1 - int(blockIdx.x / groups);
     uint32_t u = group;
     const int h = int(u % uint32_t(a.c.hd));
     u /= uint32_t(a.c.hd);
@@ -119,7 +118,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         }
         if (finder) {
             const int j = rg.slot(v0 + t * KT + lane);
-            s_off[at][lane] = f_row < 0 ? -1 : (f_row + h) * a.c.row_bytes;
+            s_off[at][lane] = f_row < 0 ? 0 : (f_row + h) * a.c.row_bytes;
             s_pos[at][lane] = a.b.positions && j >= rq.ctx && j < rq.total ? a.b.positions[rq.first + j - rq.ctx] : j;
             if constexpr (k8) {
                 f_ks = f_row < 0 ? 0.0f : a.c.scales[f_row + h];
@@ -137,6 +136,13 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     };
 
     // ---- rows of a tile: memory -> registers -> LDS ----
+    // A slot that lies in no page reads the plane's first row, a lane past the
+    // row's end its first piece: what comes of the former is masked (store, use),
+    // of the latter multiplied by q's zeros or not written.
+    static_assert(S::kKUnits % kWg == 0 || S::kKUnits < kWg, "units");
+    const int k_piece = tid % (DP / 8) * 8 * S::kEl, v_piece = tid % (DP / 4) * 4 * S::kEl;
+    const char* const k_base = kb + (k_piece < a.c.row_bytes ? k_piece : 0);
+    const char* const v_base = vb + (v_piece < a.c.row_bytes ? v_piece : 0);
     u32x4 kr[S::kKPer];
     uint2 vr[S::kVPer][8];
     auto load = [&](int t) {
@@ -145,8 +151,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         for (int i = 0; i < S::kKPer; ++i) {
             const int unit = tid + i * kWg;
             if (S::kKUnits % kWg && unit >= S::kKUnits) break;
-            const int key = unit / (DP / 8), at = unit % (DP / 8) * 8 * S::kEl;
-            const char* const p = kb + max(off[key], int64_t(0)) + (at < a.c.row_bytes ? at : 0);
+            const char* const p = k_base + off[unit / (DP / 8)];
             if constexpr (k8) {
                 const uint2 w = *reinterpret_cast<const uint2*>(p);
                 kr[i].x = w.x, kr[i].y = w.y;
@@ -158,12 +163,10 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         for (int i = 0; i < S::kVPer; ++i) {
             const int unit = tid + i * kWg;
             if (S::kVUnits % kWg && unit >= S::kVUnits) break;
-            const int kg = unit / (DP / 4), at = unit % (DP / 4) * 4 * S::kEl;
-            const int first = (kg >> 1) * 16 + (kg & 1) * 4;
-            const int past = at < a.c.row_bytes ? at : 0;
+            const int kg = unit / (DP / 4), first = (kg >> 1) * 16 + (kg & 1) * 4;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const char* const p = vb + max(off[first + (e & 3) + (e >> 2) * 8], int64_t(0)) + past;
+                const char* const p = v_base + off[first + (e & 3) + (e >> 2) * 8];
                 if constexpr (k8)
                     vr[i][e].x = *reinterpret_cast<const uint32_t*>(p);
                 else
@@ -261,33 +264,51 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         }
         // scores; element i of s[e] is slot 32 e + 8 (i / 4) + 4 half + i % 4
         float fresh_ref = 0.0f;
+        if constexpr (k8) {
 #pragma unroll
-        for (int e = 0; e < ST; ++e)
+            for (int e = 0; e < ST; ++e)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int at = 32 * e + 8 * b + 4 * half;
-                f32x4 ks = {1, 1, 1, 1};
-                if constexpr (k8) ks = *reinterpret_cast<const f32x4*>(&s_ks[ring][at]);
-                if constexpr (kRef) {
-                    const f32x4 vs = *reinterpret_cast<const f32x4*>(&s_vs[ring][at]);
+                for (int b = 0; b < 4; ++b) {
+                    const int at = 32 * e + 8 * b + 4 * half;
+                    const f32x4 ks = *reinterpret_cast<const f32x4*>(&s_ks[ring][at]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float y = __builtin_fabsf(vs[i]);
-                        fresh_ref = fmaxf(fresh_ref, y < INFINITY ? y : 0.0f);
+                    for (int i = 0; i < 4; ++i) s[e][4 * b + i] *= ks[i];
+                    if constexpr (kRef) {
+                        const f32x4 vs = *reinterpret_cast<const f32x4*>(&s_vs[ring][at]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float y = __builtin_fabsf(vs[i]);
+                            fresh_ref = fmaxf(fresh_ref, y < INFINITY ? y : 0.0f);
+                        }
                     }
                 }
-                if constexpr (!kGeneral) {
+        }
+        float to_x2 = sc.c2;                     // what s is still to be multiplied by
+        if constexpr (kGeneral) {
+            to_x2 = 1.0f;
+            const int j0 = rg.slot(v0 + t * KT);
+            if (sc.cap2 == 0.0f && (!a.b.positions || j0 + KT <= rq.ctx) && __all(qpos - j0 >= KT)) {
+                // a bias alone, all slots before the token: linear in the slot
+                const float first = slope2 * static_cast<float>(j0 + 4 * half - qpos);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[e][4 * b + i] *= k8 ? ks[i] * sc.c2 : sc.c2;
-                } else {
-                    const int4 pos = *reinterpret_cast<const int4*>(&s_pos[ring][at]);
-                    const int p[4] = {pos.x, pos.y, pos.z, pos.w};
+                for (int e = 0; e < ST; ++e)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[e][4 * b + i] = general_score(sc, k8 ? s[e][4 * b + i] * ks[i] : s[e][4 * b + i],
-                                                        slope2, qpos - p[i]);
-                }
+                    for (int i = 0; i < 16; ++i)
+                        s[e][i] = __builtin_fmaf(s[e][i], sc.c2,
+                                                 __builtin_fmaf(slope2, float(32 * e + 8 * (i >> 2) + (i & 3)), first));
+            } else {
+#pragma unroll
+                for (int e = 0; e < ST; ++e)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const int4 pos = *reinterpret_cast<const int4*>(&s_pos[ring][32 * e + 8 * b + 4 * half]);
+                        const int p[4] = {pos.x, pos.y, pos.z, pos.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            s[e][4 * b + i] = general_score(sc, s[e][4 * b + i], slope2, qpos - p[i]);
+                    }
             }
+        }
         uint64_t mine = ~uint64_t(0);
         if (!whole) {
             mine = seen_by_me(t);
@@ -302,6 +323,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         for (int e = 0; e < ST; ++e)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[e][i]);
+        if constexpr (!kGeneral) top *= to_x2;
         if constexpr (kRef) {
             fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 32));
             const uint32_t e = (__float_as_uint(fresh_ref) + 0x7FFFFFu) & 0x7F800000u;
@@ -329,7 +351,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 float p[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(s[e][4 * b + i] - base);
+                    p[i] = __builtin_amdgcn_exp2f(kGeneral ? s[e][4 * b + i] - base
+                                                           : __builtin_fmaf(s[e][4 * b + i], to_x2, -base));
                     l += p[i];
                 }
                 if constexpr (k8) {
@@ -459,7 +482,7 @@ int go_as(const AttendArgs& a, const AttendPlan& p, void* stream)
 {
     const int64_t groups = int64_t(a.c.num_requests) * a.splits * a.c.hd;
     kvx_attend_rows_kernel<kBf16, kCodes, DP, NW, kGeneral>
-        <<<dim3(uint32_t((groups + kXcds - 1) / kXcds * kXcds * p.row_tiles)), dim3(64 * NW), 0,
+        <<<dim3(uint32_t(groups * p.row_tiles)), dim3(64 * NW), 0,
            static_cast<hipStream_t>(stream)>>>(a, p.row_tiles);
     return int(hipGetLastError());
 }
@@ -467,7 +490,7 @@ int go_as(const AttendArgs& a, const AttendPlan& p, void* stream)
 template <bool kBf16, int kCodes, int DP, int NW>
 int go(const AttendArgs& a, const AttendPlan& p, void* stream)
 {
-    return a.softcap > 0.0f || a.slopes ? go_as<kBf16, kCodes, DP, NW, true>(a, p, stream)
+    return general_scores(a) ? go_as<kBf16, kCodes, DP, NW, true>(a, p, stream)
                                         : go_as<kBf16, kCodes, DP, NW, false>(a, p, stream);
 }
 

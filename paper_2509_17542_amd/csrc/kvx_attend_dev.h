@@ -205,11 +205,16 @@ __device__ __forceinline__ Range range_of(const AttendArgs& a, const Request& rq
     return g;
 }
 
-// Which of the 64 slots from j0 on a token sees; pos: the slots' positions
-// (read for new tokens' slots where positions are given), valid: those that lie
-// in a page.
+// The position of slot j.
+__device__ __forceinline__ int place_of(const AttendArgs& a, const Request& rq, int j)
+{
+    return a.b.positions && j >= rq.ctx && j < rq.total ? a.b.positions[rq.first + j - rq.ctx] : j;
+}
+
+// Which of the 64 slots from j0 on a token sees; valid: those that lie in a
+// page.
 __device__ __forceinline__ uint64_t seen_of(const AttendArgs& a, const Request& rq, int r, int i, int qp,
-                                            int j0, const int32_t* pos, uint64_t valid)
+                                            int j0, uint64_t valid)
 {
     uint64_t m;
     if (!a.b.tree) {
@@ -238,7 +243,7 @@ __device__ __forceinline__ uint64_t seen_of(const AttendArgs& a, const Request& 
             const uint64_t old = low_bits(rq.ctx - j0);
             m &= ~(out & old);
             for (int k = max(0, rq.ctx - j0); k < min(64, rq.total - j0); ++k)
-                if (int64_t(qp) - pos[k] >= a.window) m &= ~(uint64_t(1) << k);
+                if (int64_t(qp) - place_of(a, rq, j0 + k) >= a.window) m &= ~(uint64_t(1) << k);
         }
     }
     if (a.prefix) m |= low_bits(max(a.prefix[r], 0) - j0);
@@ -271,13 +276,16 @@ __device__ __forceinline__ ScoreArgs score_args(const AttendArgs& a)
     return s;
 }
 
-// a product (times its key's scale) -> x2, capped and biased; slope2 is the
-// head's slope log2(e).  tanh(y) = 1 - 2 / (exp(2 y) + 1).
+// A product (times its key's scale), capped: tanh(y) = 1 - 2 / (exp(2 y) + 1).
+__device__ __forceinline__ float capped(const ScoreArgs& s, float dot)
+{
+    return s.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * s.to_cap) + 1.0f));
+}
+
+// The product's x2, capped and biased; slope2 is the head's slope log2(e).
 __device__ __forceinline__ float general_score(const ScoreArgs& s, float dot, float slope2, int distance)
 {
-    float x = dot * s.c2;
-    if (s.cap2 > 0.0f)
-        x = s.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * s.to_cap) + 1.0f));
+    const float x = s.cap2 > 0.0f ? capped(s, dot) : dot * s.c2;
     return x - slope2 * static_cast<float>(distance < 0 ? -distance : distance);
 }
 

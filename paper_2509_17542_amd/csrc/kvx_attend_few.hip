@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
     };
     // what row tile rt sees of it, bit 16 e + i: slot 16 e + 4 g + i
     auto seen_by = [&](int rt, int v, uint32_t valid) {
-        const uint64_t m = live[rt] ? seen_of(a, rq, r, tok[rt], qpos[rt], rg.slot(v), s_pos + v - v0, valid) : 0;
+        const uint64_t m = live[rt] ? seen_of(a, rq, r, tok[rt], qpos[rt], rg.slot(v), valid) : 0;
         return uint32_t(m) >> (4 * g);
     };
     // V's slots that lie in no page were read from another

@@ -30,7 +30,8 @@ struct Shape {
     static constexpr int kVUnits = (KT / 8) * (DP / 4);     // 4 elements of 8 slots
     static constexpr int kKPer = (kKUnits + kWg - 1) / kWg;
     static constexpr int kVPer = (kVUnits + kWg - 1) / kWg;
-    static constexpr int kRing = 4;                         // tiles whose places are known
+    static constexpr int kBatch = kWg / KT;                 // tiles whose places are looked up at once
+    static constexpr int kRing = 2 * kBatch;
 };
 
 template <bool kBf16, int kCodes, int DP, int NW, bool kGeneral>
@@ -43,10 +44,9 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     constexpr uint64_t kAll = KT == 64 ? ~uint64_t(0) : (uint64_t(1) << (KT & 63)) - 1;
     __shared__ __attribute__((aligned(16))) char s_k[2][KT * S::kKRow];
     __shared__ __attribute__((aligned(16))) char s_v[2][DP * S::kVRow];
-    __shared__ int64_t s_off[S::kRing][KT];
-    __shared__ __attribute__((aligned(16))) int32_t s_pos[S::kRing][KT];
-    __shared__ __attribute__((aligned(16))) float s_ks[k8 ? S::kRing : 1][k8 ? KT : 1];
-    __shared__ __attribute__((aligned(16))) float s_vs[k8 ? S::kRing : 1][k8 ? KT : 1];
+    __shared__ int64_t s_off[2 * kWg];
+    __shared__ __attribute__((aligned(16))) float s_ks[k8 ? 2 * kWg : 1];
+    __shared__ __attribute__((aligned(16))) float s_vs[k8 ? 2 * kWg : 1];
     __shared__ uint64_t s_valid[S::kRing];
     __shared__ int s_special;
 
@@ -102,36 +102,33 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 
     if (tid == 0) s_special = 0;
 
-    // ---- places: the first wave looks them up, a lane to each slot of a tile ----
-    const bool finder = wave == 0 && lane < KT;
+    // ---- places: a slot to each lane, kBatch tiles at a time ----
+    // Looked up at the start of the batch before, noted at its end; 8-bit scales
+    // are read from there on and noted one tile later.
     int64_t f_row = -1;
     float f_ks = 0.0f, f_vs = 0.0f;
-    auto look_up = [&](int t) {
-        const int v = v0 + t * KT + lane, j = rg.slot(v);
-        f_row = finder && v < v1 && j < rq.total ? slot_row(a.c, r, j) : -1;
+    auto look_up = [&](int batch) {
+        const int v = v0 + batch * kWg + tid, j = rg.slot(v);
+        f_row = v < v1 && j < rq.total ? slot_row(a.c, r, j) : -1;
     };
-    auto note_places = [&](int t) {
-        const int at = t & (S::kRing - 1);
-        if (wave == 0) {
-            const uint64_t valid = __ballot(f_row >= 0);
-            if (lane == 0) s_valid[at] = valid;
+    auto note_places = [&](int batch) {
+        const int at = (batch & 1) * kWg + tid;
+        const uint64_t valid = __ballot(f_row >= 0);
+        if constexpr (KT == 64) {
+            if (lane == 0) s_valid[at / KT] = valid;
+        } else {
+            if (n32 == 0) s_valid[at / KT] = uint32_t(valid >> (lane & 32));
         }
-        if (finder) {
-            const int j = rg.slot(v0 + t * KT + lane);
-            s_off[at][lane] = f_row < 0 ? 0 : (f_row + h) * a.c.row_bytes;
-            s_pos[at][lane] = a.b.positions && j >= rq.ctx && j < rq.total ? a.b.positions[rq.first + j - rq.ctx] : j;
-            if constexpr (k8) {
-                f_ks = f_row < 0 ? 0.0f : a.c.scales[f_row + h];
-                f_vs = f_row < 0 ? 0.0f : a.c.scales[a.c.plane_scales + f_row + h];
-            }
-        }
-    };
-    auto note_scales = [&](int t) {
+        s_off[at] = f_row < 0 ? 0 : (f_row + h) * a.c.row_bytes;
         if constexpr (k8) {
-            if (finder) {
-                s_ks[t & (S::kRing - 1)][lane] = f_ks;
-                s_vs[t & (S::kRing - 1)][lane] = f_vs;
-            }
+            f_ks = f_row < 0 ? 0.0f : a.c.scales[f_row + h];
+            f_vs = f_row < 0 ? 0.0f : a.c.scales[a.c.plane_scales + f_row + h];
+        }
+    };
+    auto note_scales = [&](int batch) {
+        if constexpr (k8) {
+            s_ks[(batch & 1) * kWg + tid] = f_ks;
+            s_vs[(batch & 1) * kWg + tid] = f_vs;
         }
     };
 
@@ -139,18 +136,17 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     // A slot that lies in no page reads the plane's first row, a lane past the
     // row's end its first piece: what comes of the former is masked (store, use),
     // of the latter multiplied by q's zeros or not written.
-    static_assert(S::kKUnits % kWg == 0 || S::kKUnits < kWg, "units");
+    static_assert(S::kKUnits % kWg == 0 && kWg % (DP / 4) == 0, "a thread's pieces lie at one place of the rows");
     const int k_piece = tid % (DP / 8) * 8 * S::kEl, v_piece = tid % (DP / 4) * 4 * S::kEl;
     const char* const k_base = kb + (k_piece < a.c.row_bytes ? k_piece : 0);
     const char* const v_base = vb + (v_piece < a.c.row_bytes ? v_piece : 0);
     u32x4 kr[S::kKPer];
     uint2 vr[S::kVPer][8];
     auto load = [&](int t) {
-        const int64_t* const off = s_off[t & (S::kRing - 1)];
+        const int64_t* const off = s_off + (t & (S::kRing - 1)) * KT;
 #pragma unroll
         for (int i = 0; i < S::kKPer; ++i) {
             const int unit = tid + i * kWg;
-            if (S::kKUnits % kWg && unit >= S::kKUnits) break;
             const char* const p = k_base + off[unit / (DP / 8)];
             if constexpr (k8) {
                 const uint2 w = *reinterpret_cast<const uint2*>(p);
@@ -205,7 +201,6 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
         for (int i = 0; i < S::kKPer; ++i) {
             const int unit = tid + i * kWg;
-            if (S::kKUnits % kWg && unit >= S::kKUnits) break;
             const int key = unit / (DP / 8), d = unit % (DP / 8) * 8;
             u32x4 w = kr[i];
             if constexpr (k8) w = widen8<kBf16, kCodes>(kr[i].x, kr[i].y);
@@ -216,36 +211,35 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             const int unit = tid + i * kWg;
             if (S::kVUnits % kWg && unit >= S::kVUnits) break;
             const int kg = unit / (DP / 4), d = unit % (DP / 4) * 4;
-            uint32_t found = 0;
-            if (!whole) {
+            char* const out = vs + d * S::kVRow + kg * 16;
+            if (whole && kind == 0) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4*>(out + e * S::kVRow) = column(vr[i], e);
+            } else {
                 const int first = (kg >> 1) * 16 + (kg & 1) * 4;
+                uint32_t found = 0;
+                uint2 x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    if (!(valid >> (first + (e & 3) + (e >> 2) * 8) & 1)) vr[i][e] = make_uint2(0, 0);
-                    found |= nonfinite<kBf16, kCodes>(vr[i][e].x);
-                    if constexpr (!k8) found |= nonfinite<kBf16, kCodes>(vr[i][e].y);
+                    x[e] = valid >> (first + (e & 3) + (e >> 2) * 8) & 1 ? vr[i][e] : make_uint2(0, 0);
+                    found |= nonfinite<kBf16, kCodes>(x[e].x);
+                    if constexpr (!k8) found |= nonfinite<kBf16, kCodes>(x[e].y);
                 }
-            }
-            if (__builtin_expect(kind > 0 || found, 0)) {
                 if (found && kind == 0) s_special = 1;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    *reinterpret_cast<u32x4*>(vs + (d + e) * S::kVRow + kg * 16) =
-                        classify8<kBf16>(column(vr[i], e), kind);
+                    *reinterpret_cast<u32x4*>(out + e * S::kVRow) =
+                        kind == 0 && !found ? column(x, e) : classify8<kBf16>(column(x, e), kind);
                     __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
                 }
-                continue;
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *reinterpret_cast<u32x4*>(vs + (d + e) * S::kVRow + kg * 16) = column(vr[i], e);
         }
     };
 
     auto seen_by_me = [&](int t) {
         const int ring = t & (S::kRing - 1);
         uint64_t mine = ~uint64_t(0);
-        if (live) mine = seen_of(a, rq, r, tok, qpos, rg.slot(v0 + t * KT), s_pos[ring], s_valid[ring]);
+        if (live) mine = seen_of(a, rq, r, tok, qpos, rg.slot(v0 + t * KT), s_valid[ring]);
         return mine >> (4 * half);
     };
     auto use = [&](int t) {
@@ -255,13 +249,14 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         const char* const vl = s_v[t & 1] + n32 * S::kVRow + half * 16;
         f32x16 s[ST];
 #pragma unroll
-        for (int e = 0; e < ST; ++e) {
+        for (int e = 0; e < ST; ++e)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[e][i] = 0.0f;
 #pragma unroll
-            for (int c = 0; c < DP / 16; ++c)
+        for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+            for (int e = 0; e < ST; ++e)
                 s[e] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(kl + e * 32 * S::kKRow + c * 32), q[c], s[e]);
-        }
         // scores; element i of s[e] is slot 32 e + 8 (i / 4) + 4 half + i % 4
         float fresh_ref = 0.0f;
         if constexpr (k8) {
@@ -270,11 +265,11 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     const int at = 32 * e + 8 * b + 4 * half;
-                    const f32x4 ks = *reinterpret_cast<const f32x4*>(&s_ks[ring][at]);
+                    const f32x4 ks = *reinterpret_cast<const f32x4*>(s_ks + ring * KT + at);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[e][4 * b + i] *= ks[i];
                     if constexpr (kRef) {
-                        const f32x4 vs = *reinterpret_cast<const f32x4*>(&s_vs[ring][at]);
+                        const f32x4 vs = *reinterpret_cast<const f32x4*>(s_vs + ring * KT + at);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float y = __builtin_fabsf(vs[i]);
@@ -286,26 +281,33 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         float to_x2 = sc.c2;                     // what s is still to be multiplied by
         if constexpr (kGeneral) {
             to_x2 = 1.0f;
+            float mul = sc.c2;
+            if (sc.cap2 > 0.0f) {
+                mul = 1.0f;
+#pragma unroll
+                for (int e = 0; e < ST; ++e)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[e][i] = capped(sc, s[e][i]);
+            }
             const int j0 = rg.slot(v0 + t * KT);
-            if (sc.cap2 == 0.0f && (!a.b.positions || j0 + KT <= rq.ctx) && __all(qpos - j0 >= KT)) {
-                // a bias alone, all slots before the token: linear in the slot
+            if (!a.slopes || ((!a.b.positions || j0 + KT <= rq.ctx) && __all(qpos - j0 >= KT))) {
+                // all slots before the token (or no bias): linear in the slot
                 const float first = slope2 * static_cast<float>(j0 + 4 * half - qpos);
 #pragma unroll
                 for (int e = 0; e < ST; ++e)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        s[e][i] = __builtin_fmaf(s[e][i], sc.c2,
+                        s[e][i] = __builtin_fmaf(s[e][i], mul,
                                                  __builtin_fmaf(slope2, float(32 * e + 8 * (i >> 2) + (i & 3)), first));
             } else {
 #pragma unroll
                 for (int e = 0; e < ST; ++e)
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const int4 pos = *reinterpret_cast<const int4*>(&s_pos[ring][32 * e + 8 * b + 4 * half]);
-                        const int p[4] = {pos.x, pos.y, pos.z, pos.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            s[e][4 * b + i] = general_score(sc, s[e][4 * b + i], slope2, qpos - p[i]);
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = j0 + 32 * e + 8 * (i >> 2) + 4 * half + (i & 3);
+                        const int distance = qpos - place_of(a, rq, j);
+                        s[e][i] = s[e][i] * mul - slope2 * static_cast<float>(distance < 0 ? -distance : distance);
+                        __builtin_amdgcn_sched_barrier(0);  // one at a time: few tiles come here
                     }
             }
         }
@@ -356,7 +358,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     l += p[i];
                 }
                 if constexpr (k8) {
-                    const f32x4 vs = *reinterpret_cast<const f32x4*>(&s_vs[ring][32 * e + 8 * b + 4 * half]);
+                    const f32x4 vs = *reinterpret_cast<const f32x4*>(s_vs + ring * KT + 32 * e + 8 * b + 4 * half);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[i] *= kRef ? vs[i] * per_ref : vs[i];
                     if (!whole) {
@@ -382,29 +384,28 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     if (tiles > 0) {
         look_up(0);
         note_places(0);
-        note_scales(0);
-        look_up(1);
-        note_places(1);
-        look_up(2);
         __syncthreads();
         load(0);
         for (int t = 0; t < tiles; ++t) {
+            const int batch = t / S::kBatch, phase = t % S::kBatch;
             store(t, 0);
-            note_scales(t + 1);
-            note_places(t + 2);
-            look_up(t + 3);
+            if (phase == 0) note_scales(batch);
+            if (phase == S::kBatch - 1) note_places(batch + 1);
             __syncthreads();
-            if (t + 1 < tiles) load(t + 1);
+            load(min(t + 1, tiles - 1));         // the last again: nothing waits for it
+            if (phase == 0) look_up(batch + 1);
             use(t);
         }
         __syncthreads();
         if (__builtin_expect(s_special, 0)) {
             // the tiles that not every row sees whole again: which sums had infinities or NaN
             for (int t = 0; t < tiles; ++t) {
-                __syncthreads();
-                look_up(t);
-                note_places(t);
-                __syncthreads();
+                if (t % S::kBatch == 0) {
+                    __syncthreads();
+                    look_up(t / S::kBatch);
+                    note_places(t / S::kBatch);
+                    __syncthreads();
+                }
                 if (whole_tile(t)) continue;
                 const uint64_t mine = live ? seen_by_me(t) : 0;
                 for (int kind = 1; kind <= 3; ++kind) {

@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
         const int qpos = a.b.positions ? a.b.positions[token] : rq.ctx + tok;
         const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
         uint64_t mine = live && lse != -INFINITY ? ~uint64_t(0) : 0;
-        if (!whole && mine) mine = seen_of(a, rq, r, tok, qpos, j0, s_pos[wave], valid);
+        if (!whole && mine) mine = seen_of(a, rq, r, tok, qpos, j0, valid);
         mine >>= 4 * g;
         constexpr uint64_t kOwn = 0x000F000F000F000Full;
         const bool all = __all((mine & kOwn) == kOwn);

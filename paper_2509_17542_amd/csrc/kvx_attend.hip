@@ -10,52 +10,80 @@ namespace {
 
 // ---- splits joined -------------------------------------------------------------
 //
-// One workgroup per (token, query head): the sums of its splits, each relative
-// to its own reference, brought to the largest and added; always in the same
-// order.
-template <bool kBf16>
-__global__ void __launch_bounds__(256) kvx_join_kernel(const AttendArgs a)
+// The sums of a (token, query head)'s splits, each relative to its own reference,
+// are brought to the largest and added, always in the same order.  A wave to
+// each pair, or a workgroup's four where there are many splits; a split's sum is
+// read 16 bytes a lane, as many splits at once as lanes allow.
+template <bool kBf16, int kWaves>
+__global__ void __launch_bounds__(256) kvx_join_kernel(const AttendArgs a, int lg_lanes)
 {
-    __shared__ float s_part[4][256], s_red[4], s_sum[4];
+    __shared__ __attribute__((aligned(16))) float s_acc[4][256];
+    __shared__ float s_top[4], s_sum[4];
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-    const int64_t at = blockIdx.x, pairs = int64_t(a.b.total_tokens) * a.q_heads;
+    const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
+    const int64_t at = kWaves == 4 ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + wave;
+    if (at >= pairs) return;
+    const int part = kWaves == 4 ? wave : 0;
     const int token = int(at / a.q_heads), head = int(at - int64_t(token) * a.q_heads);
     const int r = request_at(a.b.starts, a.c.num_requests, token);
     if (r < 0 || r >= a.c.num_requests) return;
     const Request rq = request_of(a.c, a.b, r);
     if (token - rq.first >= rq.n) return;
     const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
+    // this wave's splits: [begin, end)
+    const int begin = a.splits * part / kWaves, end = a.splits * (part + 1) / kWaves;
     float top = -INFINITY;
-    for (int s = threadIdx.x; s < a.splits; s += 256) top = fmaxf(top, ml[s * pairs + at].x);
+    for (int s = begin + lane; s < end; s += 64) top = fmaxf(top, ml[s * pairs + at].x);
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if (lane == 0) s_red[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+    if constexpr (kWaves == 4) {
+        if (lane == 0) s_top[wave] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    }
+    const int D = a.c.dim, lanes = 1 << lg_lanes, d = 4 * (lane & (lanes - 1)), step = 64 >> lg_lanes;
     float acc[4] = {}, total = 0.0f;
-    const int D = a.c.dim, d = 4 * lane;
-    for (int s = wave; s < a.splits; s += 4) {
-        const float2 v = ml[s * pairs + at];
-        if (v.x == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(v.x - top);
-        total += v.y * f;
-        if (d < D) {
-            const float4 x = *reinterpret_cast<const float4*>(a.part_o + (s * pairs + at) * D + d);
-            acc[0] += x.x * f, acc[1] += x.y * f, acc[2] += x.z * f, acc[3] += x.w * f;
+    for (int s0 = begin; s0 < end; s0 += 64) {
+        const float2 v = s0 + lane < end ? ml[(s0 + lane) * pairs + at] : make_float2(-INFINITY, 0.0f);
+        const float f = v.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(v.x - top);
+        total += f == 0.0f ? 0.0f : v.y * f;
+        const uint64_t some = __ballot(f != 0.0f);
+        const int n = some ? 64 - __builtin_clzll(some) : 0;
+        const float* const from = a.part_o + (int64_t(s0) * pairs + at) * D + (d < D ? d : 0);
+        for (int s = 0; s < n; s += 4 * step) {
+            float4 x[4];
+            float w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int mine = s + k * step + (lane >> lg_lanes);
+                w[k] = mine < n ? __shfl(f, mine & 63) : 0.0f;
+                x[k] = *reinterpret_cast<const float4*>(from + min(mine, n - 1) * pairs * D);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (w[k] != 0.0f)       // a split that saw nothing left no sum
+                    acc[0] += x[k].x * w[k], acc[1] += x[k].y * w[k], acc[2] += x[k].z * w[k], acc[3] += x[k].w * w[k];
+            }
         }
     }
-    if (lane == 0) s_sum[wave] = total;
-    for (int k = 0; k < 4; ++k) s_part[wave][4 * lane + k] = acc[k];
-    __syncthreads();
-    if (wave != 0) return;
-    total = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    if (d < D) {
-        float x[4];
+    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+    for (int o = lanes; o < 64; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] += __shfl_xor(acc[k], o);
+    if constexpr (kWaves == 4) {
+        if (lane == 0) s_sum[wave] = total;
+        if (lane < lanes) *reinterpret_cast<float4*>(&s_acc[wave][d]) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        __syncthreads();
+        if (wave != 0) return;
+        total = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+#pragma unroll
         for (int k = 0; k < 4; ++k)
-            x[k] = (s_part[0][d + k] + s_part[1][d + k] + s_part[2][d + k] + s_part[3][d + k]) * inv;
-        *reinterpret_cast<uint2*>(a.out + token * a.out_stride + int64_t(head) * D + d) =
-            total == 0.0f ? make_uint2(0, 0) : make_uint2(pack2<kBf16>(x[0], x[1]), pack2<kBf16>(x[2], x[3]));
+            acc[k] = (s_acc[0][d + k] + s_acc[1][d + k]) + (s_acc[2][d + k] + s_acc[3][d + k]);
     }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    if (lane < lanes && d < D)
+        *reinterpret_cast<uint2*>(a.out + token * a.out_stride + int64_t(head) * D + d) =
+            total == 0.0f ? make_uint2(0, 0) : make_uint2(pack2<kBf16>(acc[0] * inv, acc[1] * inv),
+                                                          pack2<kBf16>(acc[2] * inv, acc[3] * inv));
     if (a.lse && lane == 0)
         a.lse[at] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total) - kShift<kBf16>) * kLn2;
 }
@@ -66,14 +94,21 @@ int64_t plan_pairs(const AttendArgs& a, const AttendPlan& p)
     return (int64_t(a.b.total_tokens) * a.q_heads * p.splits + 3) & ~int64_t(3);
 }
 
+template <bool kBf16, int kWaves>
+int join_as(const AttendArgs& a, void* stream)
+{
+    const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
+    int lg_lanes = 0;
+    while ((4 << lg_lanes) < a.c.dim) ++lg_lanes;
+    kvx_join_kernel<kBf16, kWaves><<<dim3(uint32_t(kWaves == 4 ? pairs : (pairs + 3) / 4)), dim3(256), 0,
+                                     static_cast<hipStream_t>(stream)>>>(a, lg_lanes);
+    return int(hipGetLastError());
+}
+
 int join(const AttendArgs& a, bool bf, void* stream)
 {
-    const dim3 grid(uint32_t(a.b.total_tokens) * uint32_t(a.q_heads));
-    if (bf)
-        kvx_join_kernel<true><<<grid, dim3(256), 0, static_cast<hipStream_t>(stream)>>>(a);
-    else
-        kvx_join_kernel<false><<<grid, dim3(256), 0, static_cast<hipStream_t>(stream)>>>(a);
-    return int(hipGetLastError());
+    if (a.splits > 32) return bf ? join_as<true, 4>(a, stream) : join_as<false, 4>(a, stream);
+    return bf ? join_as<true, 1>(a, stream) : join_as<false, 1>(a, stream);
 }
 
 }  // namespace
@@ -99,11 +134,17 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
     p.few = p.rows <= 32;
     p.tile_rows = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
-    p.chunk = 512;
-    if (!p.few) {
+    if (p.few) {
+        p.chunk = 512;
+    } else {
+        // Rows fill the card by themselves from about 3 workgroups per two of a CU's places on
+        // (chunks of 1024..2048 tokens: 810 us in one split, 1043 in splits of 2048 slots, whose
+        // sums have to be written and joined); fewer are split, the bounds counting requests
+        // shorter than the longest as idle workgroups (trees of 16..64 nodes over 2048..16384
+        // slots: 687 us in one split, 403 with 2048 slots, 392 with 1024, 433 with 512).
         const int64_t groups = int64_t(c.num_requests) * c.num_kv_heads * p.row_tiles;
-        const int64_t want = std::max<int64_t>(1, 1024 / groups);
-        p.chunk = std::max(512, int((b.max_context + want - 1) / want + 63) & ~63);
+        const int64_t want = groups >= 768 ? 1 : (4096 + groups - 1) / groups;
+        p.chunk = std::max(1024, int((b.max_context + want - 1) / want + 63) & ~63);
     }
     p.splits = (b.max_context + p.chunk - 1) / p.chunk;
     return p;

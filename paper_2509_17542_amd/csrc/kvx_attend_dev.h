@@ -276,16 +276,18 @@ __device__ __forceinline__ ScoreArgs score_args(const AttendArgs& a)
     return s;
 }
 
-// A product (times its key's scale), capped: tanh(y) = 1 - 2 / (exp(2 y) + 1).
-__device__ __forceinline__ float capped(const ScoreArgs& s, float dot)
+// softcap tanh(y) in units of log2, plus `more`; e2y is y 2 log2(e):
+// tanh(y) = 1 - 2 / (exp(2 y) + 1).
+__device__ __forceinline__ float capped(const ScoreArgs& s, float e2y, float more)
 {
-    return s.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * s.to_cap) + 1.0f));
+    return __builtin_fmaf(-2.0f * s.cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(e2y) + 1.0f),
+                          s.cap2 + more);
 }
 
 // The product's x2, capped and biased; slope2 is the head's slope log2(e).
 __device__ __forceinline__ float general_score(const ScoreArgs& s, float dot, float slope2, int distance)
 {
-    const float x = s.cap2 > 0.0f ? capped(s, dot) : dot * s.c2;
+    const float x = s.cap2 > 0.0f ? capped(s, dot * s.to_cap, 0.0f) : dot * s.c2;
     return x - slope2 * static_cast<float>(distance < 0 ? -distance : distance);
 }
 

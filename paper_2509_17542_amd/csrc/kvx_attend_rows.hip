@@ -25,7 +25,9 @@ struct Shape {
     static constexpr int KT = DP >= 256 ? 32 : 64;          // slots of a tile
     static constexpr int kEl = kCodes == kCodes16 ? 2 : 1;
     static constexpr int kKRow = DP * 2 + 16;               // LDS bytes of a slot's K
-    static constexpr int kVRow = KT * 2 + 16;               // LDS bytes of an element's V
+    // LDS bytes of an element's V: KT / 8 pieces of 8 slots, piece g at place g ^ (d / 16 % 4),
+    // so that neither the writes (a lane to every 4 elements) nor the reads meet in a bank
+    static constexpr int kVRow = KT * 2 + 16;
     static constexpr int kKUnits = KT * DP / 8;             // 8 elements of a slot
     static constexpr int kVUnits = (KT / 8) * (DP / 4);     // 4 elements of 8 slots
     static constexpr int kKPer = (kKUnits + kWg - 1) / kWg;
@@ -71,6 +73,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     const int v0 = split * a.chunk, v1 = min(v0 + a.chunk, rg.len);
     const int tiles = v1 > v0 ? (v1 - v0 + KT - 1) / KT : 0;
 
+    const bool busy = row0 + wave * 32 < rows;   // the last workgroup's last waves may only stage
     // this lane's query row
     const int row = row0 + wave * 32 + n32;
     const bool live = row < rows;
@@ -90,6 +93,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         }
     }
     const ScoreArgs sc = score_args(a);
+    const bool cap = kGeneral && sc.cap2 > 0.0f;
+    const float scale2 = cap ? sc.to_cap : sc.c2;
     f32x16 o[DTB];
 #pragma unroll
     for (int t = 0; t < DTB; ++t)
@@ -103,8 +108,9 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     if (tid == 0) s_special = 0;
 
     // ---- places: a slot to each lane, kBatch tiles at a time ----
-    // Looked up at the start of the batch before, noted at its end; 8-bit scales
-    // are read from there on and noted one tile later.
+    // Looked up a batch ahead, noted at the start of the batch before their own;
+    // 8-bit scales are read from there on and noted one tile later.  Ahead of its
+    // barrier a tile's workgroup then knows where the next tile's rows lie.
     int64_t f_row = -1;
     float f_ks = 0.0f, f_vs = 0.0f;
     auto look_up = [&](int batch) {
@@ -127,7 +133,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     };
     auto note_scales = [&](int batch) {
         if constexpr (k8) {
-            s_ks[(batch & 1) * kWg + tid] = f_ks;
+            // a key's scale, times what products are scaled by anyway
+            s_ks[(batch & 1) * kWg + tid] = f_ks * scale2;
             s_vs[(batch & 1) * kWg + tid] = f_vs;
         }
     };
@@ -142,12 +149,27 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     const char* const v_base = vb + (v_piece < a.c.row_bytes ? v_piece : 0);
     u32x4 kr[S::kKPer];
     uint2 vr[S::kVPer][8];
-    auto load = [&](int t) {
+    int64_t k_off[S::kKPer], v_off[S::kVPer][8];
+    auto places = [&](int t) {
         const int64_t* const off = s_off + (t & (S::kRing - 1)) * KT;
 #pragma unroll
+        for (int i = 0; i < S::kKPer; ++i) k_off[i] = off[(tid + i * kWg) / (DP / 8)];
+#pragma unroll
+        for (int i = 0; i < S::kVPer; ++i) {
+            const int kg = min((tid + i * kWg) / (DP / 4), KT / 8 - 1), first = (kg >> 1) * 16 + (kg & 1) * 4;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v_off[i][e] = off[first + (e & 3) + (e >> 2) * 8];
+        }
+    };
+    auto valid_of = [&](int t) {
+        const uint64_t v = s_valid[t & (S::kRing - 1)];
+        return uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(v >> 32))))) << 32 |
+               uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(v))));
+    };
+    auto load = [&]() {
+#pragma unroll
         for (int i = 0; i < S::kKPer; ++i) {
-            const int unit = tid + i * kWg;
-            const char* const p = k_base + off[unit / (DP / 8)];
+            const char* const p = k_base + k_off[i];
             if constexpr (k8) {
                 const uint2 w = *reinterpret_cast<const uint2*>(p);
                 kr[i].x = w.x, kr[i].y = w.y;
@@ -156,23 +178,19 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             }
         }
 #pragma unroll
-        for (int i = 0; i < S::kVPer; ++i) {
-            const int unit = tid + i * kWg;
-            if (S::kVUnits % kWg && unit >= S::kVUnits) break;
-            const int kg = unit / (DP / 4), first = (kg >> 1) * 16 + (kg & 1) * 4;
+        for (int i = 0; i < S::kVPer; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const char* const p = v_base + off[first + (e & 3) + (e >> 2) * 8];
+                const char* const p = v_base + v_off[i][e];
                 if constexpr (k8)
                     vr[i][e].x = *reinterpret_cast<const uint32_t*>(p);
                 else
                     vr[i][e] = *reinterpret_cast<const uint2*>(p);
             }
-        }
     };
-    auto whole_tile = [&](int t) {
+    auto whole_tile = [&](int t, uint64_t valid) {
         const int j0 = rg.slot(v0 + t * KT);
-        return j0 >= rg.all_lo && j0 + KT <= rg.all_hi && s_valid[t & (S::kRing - 1)] == kAll;
+        return j0 >= rg.all_lo && j0 + KT <= rg.all_hi && valid == kAll;
     };
     // element e of 8 slots, in the queries' type
     auto column = [&](const uint2 (&x)[8], int e) {
@@ -193,11 +211,10 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     };
     // kind 0: K, and V with its values that are not finite as 0 where not every row sees the
     // tile whole; 1 to 3: ones where V is +inf, -inf, NaN
-    auto store = [&](int t, int kind) {
+    auto store = [&](int t, uint64_t valid, int kind) {
         char* const ks = s_k[t & 1];
         char* const vs = s_v[t & 1];
-        const bool whole = whole_tile(t);
-        const uint64_t valid = s_valid[t & (S::kRing - 1)];
+        const bool whole = whole_tile(t, valid);
 #pragma unroll
         for (int i = 0; i < S::kKPer; ++i) {
             const int unit = tid + i * kWg;
@@ -211,7 +228,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             const int unit = tid + i * kWg;
             if (S::kVUnits % kWg && unit >= S::kVUnits) break;
             const int kg = unit / (DP / 4), d = unit % (DP / 4) * 4;
-            char* const out = vs + d * S::kVRow + kg * 16;
+            char* const out = vs + d * S::kVRow + (kg ^ ((d >> 4) & 3)) * 16;
             if (whole && kind == 0) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4*>(out + e * S::kVRow) = column(vr[i], e);
@@ -236,17 +253,16 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         }
     };
 
-    auto seen_by_me = [&](int t) {
-        const int ring = t & (S::kRing - 1);
+    auto seen_by_me = [&](int t, uint64_t valid) {
         uint64_t mine = ~uint64_t(0);
-        if (live) mine = seen_of(a, rq, r, tok, qpos, rg.slot(v0 + t * KT), s_valid[ring]);
+        if (live) mine = seen_of(a, rq, r, tok, qpos, rg.slot(v0 + t * KT), valid);
         return mine >> (4 * half);
     };
-    auto use = [&](int t) {
+    auto use = [&](int t, uint64_t valid) {
         const int ring = t & (S::kRing - 1);
-        const bool whole = whole_tile(t);
+        const bool whole = whole_tile(t, valid);
         const char* const kl = s_k[t & 1] + n32 * S::kKRow + half * 16;
-        const char* const vl = s_v[t & 1] + n32 * S::kVRow + half * 16;
+        const char* const vl = s_v[t & 1] + n32 * S::kVRow + (half ^ (n32 >> 4)) * 16;
         f32x16 s[ST];
 #pragma unroll
         for (int e = 0; e < ST; ++e)
@@ -257,9 +273,13 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
             for (int e = 0; e < ST; ++e)
                 s[e] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(kl + e * 32 * S::kKRow + c * 32), q[c], s[e]);
-        // scores; element i of s[e] is slot 32 e + 8 (i / 4) + 4 half + i % 4
+        // Scores relative to the row's reference so far; element i of s[e] is slot
+        // 32 e + 8 (i / 4) + 4 half + i % 4.
+        float base = (m == -INFINITY ? 0.0f : m) - kShift<kBf16>;
         float fresh_ref = 0.0f;
+        float by = scale2;                       // what the products are still to be multiplied by
         if constexpr (k8) {
+            by = 1.0f;
 #pragma unroll
             for (int e = 0; e < ST; ++e)
 #pragma unroll
@@ -267,7 +287,9 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     const int at = 32 * e + 8 * b + 4 * half;
                     const f32x4 ks = *reinterpret_cast<const f32x4*>(s_ks + ring * KT + at);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[e][4 * b + i] *= ks[i];
+                    for (int i = 0; i < 4; ++i)
+                        s[e][4 * b + i] = kGeneral ? s[e][4 * b + i] * ks[i]
+                                                   : __builtin_fmaf(s[e][4 * b + i], ks[i], -base);
                     if constexpr (kRef) {
                         const f32x4 vs = *reinterpret_cast<const f32x4*>(s_vs + ring * KT + at);
 #pragma unroll
@@ -278,42 +300,49 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     }
                 }
         }
-        float to_x2 = sc.c2;                     // what s is still to be multiplied by
         if constexpr (kGeneral) {
-            to_x2 = 1.0f;
-            float mul = sc.c2;
-            if (sc.cap2 > 0.0f) {
-                mul = 1.0f;
+            const int j0 = rg.slot(v0 + t * KT);
+            const bool linear = (!a.b.positions || j0 + KT <= rq.ctx) && __all(qpos - j0 >= KT);
+            const float first = slope2 * static_cast<float>(j0 + 4 * half - qpos) - base;
+            if (cap) {
 #pragma unroll
                 for (int e = 0; e < ST; ++e)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[e][i] = capped(sc, s[e][i]);
-            }
-            const int j0 = rg.slot(v0 + t * KT);
-            if (!a.slopes || ((!a.b.positions || j0 + KT <= rq.ctx) && __all(qpos - j0 >= KT))) {
-                // all slots before the token (or no bias): linear in the slot
-                const float first = slope2 * static_cast<float>(j0 + 4 * half - qpos);
+                    for (int i = 0; i < 16; ++i) s[e][i] = capped(sc, s[e][i] * by, -base);
+            } else if (!a.slopes || !linear) {
+#pragma unroll
+                for (int e = 0; e < ST; ++e)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[e][i] = __builtin_fmaf(s[e][i], by, -base);
+            } else {
+                // a bias alone, all slots before the token: linear in the slot
 #pragma unroll
                 for (int e = 0; e < ST; ++e)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        s[e][i] = __builtin_fmaf(s[e][i], mul,
+                        s[e][i] = __builtin_fmaf(s[e][i], by,
                                                  __builtin_fmaf(slope2, float(32 * e + 8 * (i >> 2) + (i & 3)), first));
-            } else {
+            }
+            if (a.slopes && (cap || !linear)) {
 #pragma unroll
                 for (int e = 0; e < ST; ++e)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int j = j0 + 32 * e + 8 * (i >> 2) + 4 * half + (i & 3);
                         const int distance = qpos - place_of(a, rq, j);
-                        s[e][i] = s[e][i] * mul - slope2 * static_cast<float>(distance < 0 ? -distance : distance);
-                        __builtin_amdgcn_sched_barrier(0);  // one at a time: few tiles come here
+                        s[e][i] -= slope2 * static_cast<float>(distance < 0 ? -distance : distance);
+                        __builtin_amdgcn_sched_barrier(0);  // one at a time
                     }
             }
+        } else if constexpr (!k8) {
+#pragma unroll
+            for (int e = 0; e < ST; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[e][i] = __builtin_fmaf(s[e][i], by, -base);
         }
         uint64_t mine = ~uint64_t(0);
         if (!whole) {
-            mine = seen_by_me(t);
+            mine = seen_by_me(t, valid);
 #pragma unroll
             for (int e = 0; e < ST; ++e)
 #pragma unroll
@@ -325,25 +354,28 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         for (int e = 0; e < ST; ++e)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[e][i]);
-        if constexpr (!kGeneral) top *= to_x2;
         if constexpr (kRef) {
             fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 32));
             const uint32_t e = (__float_as_uint(fresh_ref) + 0x7FFFFFu) & 0x7F800000u;
             fresh_ref = __uint_as_float(min(max(e, 0x00800000u), 0x7E800000u));
         }
         const bool grow = kRef && fresh_ref > ref;
-        if (__any(top > m + kSlack) || grow) {
+        if (__any(top > (m == -INFINITY ? -INFINITY : kSlack + kShift<kBf16>)) || grow) {
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float to = fmaxf(m, top);
+            const float to = fmaxf(m, top + base);
             float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            const float by2 = base - ((to == -INFINITY ? 0.0f : to) - kShift<kBf16>);
             l *= alpha;
             m = to;
             if (grow) alpha *= ref / fresh_ref;
 #pragma unroll
             for (int t2 = 0; t2 < DTB; ++t2) o[t2] *= alpha;
+#pragma unroll
+            for (int e = 0; e < ST; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[e][i] += by2;
         }
         if constexpr (kRef) ref = fmaxf(ref, fresh_ref);
-        const float base = (m == -INFINITY ? 0.0f : m) - kShift<kBf16>;
         const float per_ref = kRef ? 1.0f / ref : 1.0f;
         u32x4 pf[ST][2];
 #pragma unroll
@@ -353,8 +385,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 float p[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(kGeneral ? s[e][4 * b + i] - base
-                                                           : __builtin_fmaf(s[e][4 * b + i], to_x2, -base));
+                    p[i] = __builtin_amdgcn_exp2f(s[e][4 * b + i]);
                     l += p[i];
                 }
                 if constexpr (k8) {
@@ -377,24 +408,32 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int t2 = 0; t2 < DTB; ++t2)
-                    o[t2] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + b * 32),
+                    o[t2] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + (b ^ (t2 & 1)) * 32),
                                           pf[e][b], o[t2]);
     };
 
     if (tiles > 0) {
         look_up(0);
         note_places(0);
+        note_scales(0);
+        look_up(1);
         __syncthreads();
-        load(0);
+        places(0);
+        uint64_t valid = valid_of(0);
+        load();
         for (int t = 0; t < tiles; ++t) {
             const int batch = t / S::kBatch, phase = t % S::kBatch;
-            store(t, 0);
-            if (phase == 0) note_scales(batch);
-            if (phase == S::kBatch - 1) note_places(batch + 1);
+            const int next = min(t + 1, tiles - 1);  // the last again: nothing waits for it
+            store(t, valid, 0);
+            if (phase == 1) note_scales(batch + 1);
+            places(next);
+            const uint64_t next_valid = valid_of(next);
+            if (phase == 0) note_places(batch + 1);
             __syncthreads();
-            load(min(t + 1, tiles - 1));         // the last again: nothing waits for it
-            if (phase == 0) look_up(batch + 1);
-            use(t);
+            load();
+            if (phase == 0) look_up(batch + 2);
+            if (busy) use(t, valid);
+            valid = next_valid;
         }
         __syncthreads();
         if (__builtin_expect(s_special, 0)) {
@@ -406,13 +445,15 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     note_places(t / S::kBatch);
                     __syncthreads();
                 }
-                if (whole_tile(t)) continue;
-                const uint64_t mine = live ? seen_by_me(t) : 0;
+                valid = valid_of(t);
+                if (whole_tile(t, valid)) continue;
+                const uint64_t mine = live ? seen_by_me(t, valid) : 0;
                 for (int kind = 1; kind <= 3; ++kind) {
-                    load(t);
-                    store(t, kind);
+                    places(t);
+                    load();
+                    store(t, valid, kind);
                     __syncthreads();
-                    const char* const vl = s_v[t & 1] + n32 * S::kVRow + half * 16;
+                    const char* const vl = s_v[t & 1] + n32 * S::kVRow + (half ^ (n32 >> 4)) * 16;
 #pragma unroll
                     for (int t2 = 0; t2 < DTB; ++t2) {
                         f32x16 count;
@@ -426,7 +467,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                                 const uint32_t two = uint32_t(mine >> (16 * e + 8 * (w >> 1) + 2 * (w & 1))) & 3u;
                                 seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
                             }
-                            count = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 32),
+                            count = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + (e >> 1) * 64 + ((e ^ t2) & 1) * 32),
                                                   seen, count);
                         }
 #pragma unroll

@@ -84,13 +84,14 @@ struct MoveArgs {
     const int32_t* index;        // evict: [layer][request][head][stride]; commit: [request][stride]
     int32_t stride;
     int32_t num_layers;
-    // evict: rows of request r are min(lens[r], stride) where lens[r] > stride, else none;
-    // commit: new_lens[r] - contexts[r], from slot contexts[r] on
+    int32_t max_len;
+    int32_t lg_lanes;            // log2 of the lanes that a row takes
+    // evict: `stride` rows of request r where lens[r] is above that, else none; commit: a path of
+    // counts[r] entries or fewer, from slot contexts[r] on, whose end goes to new_lens[r]
     const int32_t* lens;
     const int32_t* contexts;
-    const int32_t* new_lens;
-    int32_t max_len;
-    int32_t pad;
+    const int32_t* counts;
+    int32_t* new_lens;
 };
 
 struct AttendArgs {

@@ -3,6 +3,8 @@
 // the move of rows up their request, shared by kvx_evict and kvx_commit.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "kvx_ops_dev.h"
 
 namespace kvx {
@@ -12,7 +14,7 @@ constexpr int kWg = 256;
 
 // ---- append ------------------------------------------------------------------
 
-// Maximum over each aligned group of 2^lg lanes, lg <= 5.
+// Maximum over each aligned group of 2^lg lanes, lg <= 5, all of them active.
 __device__ __forceinline__ float lanes_max(float m, int lg)
 {
     for (int o = 1; o < (1 << lg); o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
@@ -38,95 +40,139 @@ __device__ __forceinline__ uint32_t code8(float x, float s)
     return sign | code;
 }
 
-// One workgroup per token.  The turns of its pairs (cosine and sine of the
-// fp32 angle, reduced in fp64 to a fraction of a turn) are computed once into
-// LDS and shared by its q_heads + Hd turned heads; a power-of-two group of
-// lanes covers a head, 8 elements (16 bytes) a lane.
-template <bool kBf16, int kCache>
+enum Pairing : int { kHalves = 0, kInterleaved = 1, kAnyHalves = 2 };
+
+// 8 elements of 16 bits -> fp32
+template <bool kBf16>
+__device__ __forceinline__ void widen(const uint4& w, float (&x)[8])
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = value16<kBf16>((u[e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
+}
+
+template <bool kBf16>
+__device__ __forceinline__ uint4 narrow(const float (&x)[8])
+{
+    uint32_t u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = bits16<kBf16>(x[2 * k]) | bits16<kBf16>(x[2 * k + 1]) << 16;
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// A workgroup takes kTokens tokens: their turns (cosine and sine of the fp32
+// angles, reduced in fp64 to a fraction of a turn) go to LDS once for all heads,
+// and each token's place in the cache is looked up by one wave.  A power-of-two
+// group of lanes then covers a head, 8 elements (16 bytes) a lane, whose turns
+// stay in registers for all of a token's heads; the element that a turn pairs
+// with lies in the lane (interleaved) or is read again, out of the cache
+// (halves; pairs that do not fill whole lanes element by element).  Bound by memory for
+// prompts and by its chain of lookups for single tokens.
+template <bool kBf16, int kCache, int kPairing, int kTokens>
 __global__ void __launch_bounds__(kWg) kvx_append_kernel(const AppendArgs a)
 {
-    __shared__ float2 turn[128];
-    const int t = int(blockIdx.x);
-    const int D = a.c.dim, P = a.pairs;
-    for (int i = threadIdx.x; i < P; i += kWg) {
+    __shared__ float2 s_turn[kTokens][128];
+    __shared__ int64_t s_row[kTokens];
+    const int t0 = int(blockIdx.x) * kTokens, wave = int(threadIdx.x) >> 6;
+    const int D = a.c.dim, P = a.pairs, N = a.b.total_tokens;
+    for (int u = threadIdx.x; u < kTokens * P; u += kWg) {
+        const int k = u / P, i = u - k * P, t = t0 + k;
+        if (t >= N) break;
         int axis = 0;
 #pragma unroll
         for (int s = 0; s < 3; ++s) axis += i >= a.sec_end[s];
-        const float pos = static_cast<float>(a.positions[int64_t(axis) * a.b.total_tokens + t]);
+        const float pos = static_cast<float>(a.positions[int64_t(axis) * N + t]);
         const double turns = double(pos * a.inv_freq[i]) * 0.15915494309189533577;
-        const float frac = static_cast<float>(turns - rint(turns));
         float sn, cs;
-        sincospif(2.0f * frac, &sn, &cs);
-        turn[i] = make_float2(cs, sn);
+        sincospif(2.0f * static_cast<float>(turns - rint(turns)), &sn, &cs);
+        s_turn[k][i] = make_float2(cs, sn);
     }
-    const int r = request_at(a.b.starts, a.c.num_requests, t);
-    int64_t row = -1;
-    if (r >= 0 && r < a.c.num_requests) {
-        const Request rq = request_of(a.c, a.b, r);
-        const int j = rq.ctx + (t - rq.first);
-        if (t - rq.first < rq.n && j < rq.total) row = slot_row(a.c, r, j);
+    for (int k = wave; k < kTokens; k += kWg / 64) {
+        const int t = t0 + k;
+        int64_t row = -1;
+        const int r = t < N ? request_at(a.b.starts, a.c.num_requests, t) : -1;
+        if (r >= 0 && r < a.c.num_requests) {
+            const Request rq = request_of(a.c, a.b, r);
+            const int j = rq.ctx + (t - rq.first);
+            if (t - rq.first < rq.n && j < rq.total) row = slot_row(a.c, r, j);
+        }
+        if ((threadIdx.x & 63) == 0) s_row[k] = row;
     }
     __syncthreads();
-    const int per = 1 << a.lg_row;
-    const int lane = int(threadIdx.x) & (per - 1), e0 = lane * 8;
+    const int per = 1 << a.lg_row, lane = int(threadIdx.x) & (per - 1), e0 = lane * 8;
     const int rows = a.q_heads + 2 * a.c.hd;
-    for (int h0 = 0; h0 < rows; h0 += kWg >> a.lg_row) {
-        const int h = h0 + (int(threadIdx.x) >> a.lg_row);
-        const bool live = h < rows && e0 < D;
-        const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.c.hd;
-        float x[8] = {};
-        if (live) {
-            const uint16_t* src = is_q ? a.q + t * a.q_stride + int64_t(h) * D
-                                : is_v ? a.v + t * a.v_stride + int64_t(h - a.q_heads - a.c.hd) * D
-                                       : a.k + t * a.k_stride + int64_t(h - a.q_heads) * D;
+    const bool in_row = e0 < D;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = e0 + e;
-                x[e] = value16<kBf16>(src[i]);
-                if (!is_v && i < 2 * P) {
-                    int pair, other;
-                    bool second;
-                    if (a.interleaved) {
-                        pair = i >> 1, second = i & 1, other = i ^ 1;
-                    } else {
-                        second = i >= P, pair = second ? i - P : i, other = second ? i - P : i + P;
+    for (int k = 0; k < kTokens; ++k) {
+        const int64_t t = t0 + k;
+        if (t >= N) return;
+        const int64_t row = s_row[k];
+        // the turns of this lane's elements: x cs + y sn, the sign of sn with it
+        float cs[8], sn[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int i = e0 + e;
+            cs[e] = 1.0f, sn[e] = 0.0f;
+            if (i < 2 * P) {
+                const bool second = kPairing == kInterleaved ? i & 1 : i >= P;
+                const float2 x = s_turn[k][kPairing == kInterleaved ? i >> 1 : second ? i - P : i];
+                cs[e] = x.x;
+                sn[e] = second ? x.y : -x.y;
+            }
+        }
+        const bool turned = e0 < 2 * P;          // and so in the row
+        const int other = kPairing == kHalves && turned ? (e0 >= P ? e0 - P : e0 + P) : e0;
+        for (int h = int(threadIdx.x) >> a.lg_row; h < rows; h += kWg >> a.lg_row) {
+            const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.c.hd;
+            const uint16_t* const src = is_q ? a.q + t * a.q_stride + int64_t(h) * D
+                                      : is_v ? a.v + t * a.v_stride + int64_t(h - a.q_heads - a.c.hd) * D
+                                             : a.k + t * a.k_stride + int64_t(h - a.q_heads) * D;
+            // lanes past the row's end hold zeros: the row's maximum takes all of its group
+            float x[8] = {};
+            if (in_row) widen<kBf16>(*reinterpret_cast<const uint4*>(src + e0), x);
+            if (!is_v && turned) {
+                float y[8];
+                if constexpr (kPairing == kInterleaved) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+                } else if constexpr (kPairing == kHalves) {
+                    widen<kBf16>(*reinterpret_cast<const uint4*>(src + other), y);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int i = e0 + e;
+                        y[e] = i < 2 * P ? value16<kBf16>(src[i >= P ? i - P : i + P]) : 0.0f;
                     }
-                    const float y = value16<kBf16>(src[other]);
-                    const float2 cs = turn[pair];
-                    x[e] = second ? x[e] * cs.x + y * cs.y : x[e] * cs.x - y * cs.y;
                 }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e0 + e < 2 * P) x[e] = x[e] * cs[e] + y[e] * sn[e];
             }
-        }
-        // every lane has read its elements before q_out, which may be q, is written
-        __syncthreads();
-        if (is_q) {
-            if (live) {
-                uint16_t* dst = a.q_out + t * a.q_out_stride + int64_t(h) * D;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e0 + e] = uint16_t(bits16<kBf16>(x[e]));
+            if (is_q) {
+                // q_out may be q: the head's lanes, all of one wave, have read it
+                __builtin_amdgcn_wave_barrier();
+                if (in_row)
+                    *reinterpret_cast<uint4*>(a.q_out + t * a.q_out_stride + int64_t(h) * D + e0) = narrow<kBf16>(x);
+                continue;
             }
-            continue;
-        }
-        const int kv = is_v ? 1 : 0, head = h - a.q_heads - (is_v ? a.c.hd : 0);
-        char* plane = a.c.base + kv * a.c.plane_bytes;
-        if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
-            if (live && row >= 0) {
-                uint16_t* dst = reinterpret_cast<uint16_t*>(plane) + (row + head) * D;
+            const int kv = is_v ? 1 : 0, head = h - a.q_heads - (is_v ? a.c.hd : 0);
+            char* const dst = a.c.base + kv * a.c.plane_bytes + (row + head) * a.c.row_bytes;
+            if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
+                if (row >= 0 && in_row) *reinterpret_cast<uint4*>(dst + e0 * 2) = narrow<kCache == KVX_BF16>(x);
+            } else {
+                constexpr bool kE5 = kCache == KVX_FP8_E5M2;
+                float m = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e0 + e] = uint16_t(bits16<kCache == KVX_BF16>(x[e]));
-            }
-        } else {
-            constexpr bool kE5 = kCache == KVX_FP8_E5M2;
-            float m = 0.0f;
+                for (int e = 0; e < 8; ++e) m = fmaxf(m, __builtin_fabsf(x[e]));  // a NaN takes no part
+                m = lanes_max(m, a.lg_row);
+                const float s = m / (kE5 ? 57344.0f : 448.0f);
+                uint32_t w[2] = {0, 0};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = fmaxf(m, __builtin_fabsf(x[e]));  // a NaN takes no part
-            m = lanes_max(m, a.lg_row);
-            const float s = m / (kE5 ? 57344.0f : 448.0f);
-            if (live && row >= 0) {
-                uint8_t* dst = reinterpret_cast<uint8_t*>(plane) + (row + head) * D;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e0 + e] = uint8_t(code8<kE5>(x[e], s));
-                if (lane == 0) a.c.scales[kv * a.c.plane_scales + row + head] = s;
+                for (int e = 0; e < 8; ++e) w[e >> 2] |= code8<kE5>(x[e], s) << (8 * (e & 3));
+                if (row >= 0 && in_row) {
+                    *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[0], w[1]);
+                    if (lane == 0) a.c.scales[kv * a.c.plane_scales + row + head] = s;
+                }
             }
         }
     }
@@ -143,37 +189,20 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Inclusive sum over a workgroup of 256, in thread order, and the total.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* part, uint32_t& total)
-{
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t u = __shfl_up(v, o);
-        if (lane >= o) v += u;
-    }
-    __syncthreads();
-    if (lane == 63) part[wave] = v;
-    __syncthreads();
-    uint32_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int k = 0; k < kWg / 64; ++k) {
-        before += k < wave ? part[k] : 0u;
-        total += part[k];
-    }
-    return v + before;
-}
-
 // One workgroup per (layer, request, head).  The weight of the last slot that
-// stays is found by its key's four bytes, highest first: a histogram of the
-// candidates that agree with the bytes found so far, walked from the top.  Then
+// stays is found by its key, 11, 11 and 10 bits at a time: a histogram of the
+// candidates that agree with the bits found so far, walked from the top.  Then
 // one pass in slot order writes what stays; of the slots that tie with that
-// weight the first ones.
-__global__ void __launch_bounds__(kWg) kvx_select_kernel(const EvictArgs a)
+// weight the first ones, which takes a second count only where not all of them
+// stay.  The weights are read four times, all but the first from the L2.
+template <int kThreads_>
+__global__ void __launch_bounds__(kThreads_) kvx_select_kernel(const EvictArgs a)
 {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t part[kWg / 64];
-    __shared__ uint32_t s_byte, s_left;
+    constexpr int kW = kThreads_ / 64, kBins = 2048, kPer = kBins / kThreads_;
+    __shared__ uint32_t s_hist[kBins];
+    __shared__ uint32_t s_part[2][kW];
+    __shared__ uint32_t s_bin, s_left, s_same;
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
     const int lrh = int(blockIdx.x);
     const int r = (lrh / a.c.hd) % a.c.num_requests;
     const int T = min(min(max(a.lens[r], 0), a.max_len), a.c.row_slots);
@@ -181,163 +210,320 @@ __global__ void __launch_bounds__(kWg) kvx_select_kernel(const EvictArgs a)
     const float* w = a.weights + int64_t(lrh) * a.w_stride;
     float* w_out = a.weights_out + int64_t(lrh) * a.w_stride;
     int32_t* kept = a.kept + int64_t(lrh) * a.budget;
-    if (lrh < a.c.num_requests * a.c.hd && lrh % a.c.hd == 0 && threadIdx.x == 0)
-        a.new_lens[r] = keep;
+    if (lrh < a.c.num_requests * a.c.hd && lrh % a.c.hd == 0 && tid == 0) a.new_lens[r] = keep;
     if (T <= a.budget) {
-        for (int i = threadIdx.x; i < a.budget; i += kWg) {
+        for (int i = tid; i < a.budget; i += kThreads_) {
             if (i < T && w_out != w) w_out[i] = w[i];
             kept[i] = i < T ? i : -1;
         }
         return;
     }
     const int lo = a.sink, hi = T - a.recent;    // candidates; sink + recent <= budget < T
-    uint32_t left = uint32_t(a.budget - a.sink - a.recent);
-    uint32_t key = 0;                            // bytes found so far
-    if (left) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            hist[threadIdx.x] = 0;
+    uint32_t left = uint32_t(a.budget - a.sink - a.recent), same = 0;
+    uint32_t key = 0;                            // bits found so far
+    const bool any = left != 0;
+    if (any) {
+        for (int step = 0; step < 3; ++step) {
+            const int shift = step == 0 ? 21 : step == 1 ? 10 : 0;
+            const uint32_t mask = step == 2 ? 1023u : 2047u;
+            for (int b = tid; b < kBins; b += kThreads_) s_hist[b] = 0;
             __syncthreads();
-            for (int j = lo + int(threadIdx.x); j < hi; j += kWg) {
+            const int above = step == 0 ? 32 : step == 1 ? 21 : 10;
+            for (int j = lo + tid; j < hi; j += kThreads_) {
                 const uint32_t k = weight_key(w[j]);
-                if (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8)))
-                    atomicAdd(&hist[(k >> shift) & 255u], 1u);
+                if (step == 0 || (k >> above) == (key >> above)) atomicAdd(&s_hist[(k >> shift) & mask], 1u);
             }
             __syncthreads();
-            // thread i holds byte 255 - i: the inclusive sum counts the larger ones too
-            const uint32_t mine = hist[255 - threadIdx.x];
-            uint32_t total;
-            const uint32_t upto = block_scan(mine, part, total);
-            if (upto >= left && upto - mine < left) {
-                s_byte = 255u - threadIdx.x;
-                s_left = left - (upto - mine);
+            // thread i holds kPer bins from the top down
+            uint32_t mine[kPer], sum = 0;
+#pragma unroll
+            for (int b = 0; b < kPer; ++b) sum += mine[b] = s_hist[kBins - 1 - (tid * kPer + b)];
+            uint32_t upto = sum;
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t u = __shfl_up(upto, o);
+                if (lane >= o) upto += u;
+            }
+            if (lane == 63) s_part[0][wave] = upto;
+            __syncthreads();
+            for (int k = 0; k < wave; ++k) upto += s_part[0][k];
+            uint32_t before = upto - sum;
+#pragma unroll
+            for (int b = 0; b < kPer; ++b) {
+                if (before < left && before + mine[b] >= left) {
+                    s_bin = kBins - 1 - (tid * kPer + b);
+                    s_left = left - before;
+                    s_same = mine[b];
+                }
+                before += mine[b];
             }
             __syncthreads();
-            key |= s_byte << shift;
+            key |= s_bin << shift;
             left = s_left;
+            same = s_same;
             __syncthreads();
         }
     }
-    // `left` slots of weight `key` stay, and all above it
-    const bool any = a.budget > a.sink + a.recent;
+    // all slots above `key` stay and the first `left` of the `same` that equal it
+    const bool all_ties = same == left;
     uint32_t ties = 0, out = 0;
-    for (int j0 = 0; j0 < T; j0 += kWg) {
-        const int j = j0 + int(threadIdx.x);
-        const float x = j < T ? w[j] : 0.0f;
+    int turn = 0;
+    // counts a flag over the workgroup in slot order: how many before this thread, and in all
+    auto count = [&](bool flag, uint32_t& total) {
+        const uint64_t m = __ballot(flag);
+        uint32_t* const part = s_part[turn];
+        turn ^= 1;                               // the other half may still be read
+        if (lane == 0) part[wave] = uint32_t(__popcll(m));
+        __syncthreads();
+        uint32_t before = uint32_t(__popcll(m & ((uint64_t(1) << lane) - 1)));
+        total = 0;
+#pragma unroll
+        for (int k = 0; k < kW; ++k) {
+            before += k < wave ? part[k] : 0u;
+            total += part[k];
+        }
+        return before;
+    };
+    float x = tid < T ? w[tid] : 0.0f;
+    for (int j0 = 0; j0 < T; j0 += kThreads_) {
+        const int j = j0 + tid;
+        // read ahead of this round's writes: w_out may be w, and they lie below
+        const float next = j + kThreads_ < T ? w[j + kThreads_] : 0.0f;
         const bool cand = j >= lo && j < hi;
         const uint32_t k = weight_key(x);
+        bool stay = j < T && (!cand || (any && k > key));
         const bool tie = any && cand && k == key;
-        uint32_t n_ties, n_out;
-        const uint32_t rank = block_scan(tie ? 1u : 0u, part, n_ties) + ties;
-        const bool stay = j < T && (!cand || (any && k > key) || (tie && rank <= left));
-        const uint32_t at = block_scan(stay ? 1u : 0u, part, n_out) + out;
-        // w_out may be w: position at - 1 <= j, and every thread has read its weight
-        if (stay) {
-            kept[at - 1] = j;
-            w_out[at - 1] = x;
+        if (all_ties) {
+            stay |= tie;
+        } else {
+            uint32_t n;
+            const uint32_t rank = count(tie, n) + ties;
+            stay |= tie && rank < left;
+            ties += n;
         }
-        ties += n_ties;
-        out += n_out;
+        uint32_t n;
+        const uint32_t at = count(stay, n) + out;
+        out += n;
+        if (stay) {
+            kept[at] = j;
+            w_out[at] = x;                       // at <= j: read by every thread already
+        }
+        x = next;
     }
 }
 
 // ---- rows move up -------------------------------------------------------------
+//
+// A row never moves down (its source is at or above its target, both ascend), so
+// rows may move in place in order, a group at a time: all of a group's rows are
+// read before any of it is written, and a write can only hit rows that this or
+// an earlier group has read.  Pieces of 16 bytes, a power-of-two number of lanes
+// to a row, kHold pieces a lane in flight.  Bound by memory.
+constexpr int kHold = 8;
 
-// One workgroup per (layer, k/v, request, head) moves its rows in order, a
-// group of rows at a time: all of a group's rows are read, then written.  A row
-// never moves down (index[i] >= i), so a write can only hit rows that this or
-// an earlier group has read.
-template <bool kCommit>
+typedef uint32_t piece_t __attribute__((ext_vector_type(4)));
+
+// What a lane holds of a group.
+struct Held {
+    piece_t x[kHold];
+    float s[kHold];
+    int64_t to[kHold];                           // row it goes to, -1: none
+};
+
+// Every load of `v` has returned: the compiler waits for those alone, not for
+// stores that are younger.
+__device__ __forceinline__ void arrived(Held& v)
+{
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) __asm__ volatile("" : "+v"(v.x[k]), "+v"(v.s[k]));
+}
+
+// Eviction: one workgroup per (layer, k/v, request, head), whose kept slots are
+// its own.  The next group's rows are read before this one's are written, and
+// the places of the one after that looked up meanwhile.
 __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
 {
-    const int H = a.c.hd, R = a.c.num_requests;
+    __shared__ int64_t s_src[2][kWg], s_dst[2][kWg];
+    const int tid = int(threadIdx.x), H = a.c.hd, R = a.c.num_requests;
     int u = int(blockIdx.x);
     const int h = u % H;
     u /= H;
     const int r = u % R;
     u /= R;
     const int kv = u & 1, layer = u >> 1;
-    int rows, first = 0;
-    const int32_t* index;
-    if constexpr (kCommit) {
-        first = max(a.contexts[r], 0);
-        rows = min(a.new_lens[r] - first, a.stride);
-        index = a.index + int64_t(r) * a.stride;
-    } else {
-        const int T = min(min(max(a.lens[r], 0), a.max_len), a.c.row_slots);
-        rows = T > a.stride ? a.stride : 0;
-        index = a.index + ((int64_t(layer) * R + r) * H + h) * a.stride;
-    }
+    const int T = min(min(max(a.lens[r], 0), a.max_len), a.c.row_slots);
+    const int rows = T > a.stride ? a.stride : 0;
+    if (rows == 0) return;
+    const int32_t* const index = a.index + ((int64_t(layer) * R + r) * H + h) * a.stride;
     const int64_t plane = int64_t(2) * layer + kv;
-    char* base = a.c.base + plane * a.c.plane_bytes;
-    float* scales = a.c.scales ? a.c.scales + plane * a.c.plane_scales : nullptr;
-    const int chunks = a.c.row_bytes >> 4;                 // 16-byte pieces of a row
-    int lg = 0;
-    while ((1 << lg) < chunks) ++lg;
-    const int per = 1 << lg, group = kWg >> lg;
-    const int piece = int(threadIdx.x) & (per - 1);
-    for (int i0 = 0; i0 < rows; i0 += group) {
-        const int i = i0 + (int(threadIdx.x) >> lg);
-        int64_t src = -1, dst = -1;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        float s = 0.0f;
-        if (i < rows && piece < chunks) {
-            const int from = index[i];
-            if (from > i && first + from < a.c.row_slots) {
+    char* const base = a.c.base + plane * a.c.plane_bytes;
+    float* const scales = a.c.scales ? a.c.scales + plane * a.c.plane_scales : nullptr;
+    const int pieces = a.c.row_bytes >> 4, lg = a.lg_lanes;
+    const int sets = min(kWg >> lg, kWg / kHold), group = sets * kHold;
+    const int set = tid >> lg, piece = tid & ((1 << lg) - 1);
+    const bool mine = set < sets && piece < pieces;
+    const int64_t at = min(piece, pieces - 1) * 16;
+
+    auto look_up = [&](int i0, int side) {
+        if (tid < group) {
+            const int i = i0 + tid;
+            int64_t src = -1, dst = -1;
+            if (i < rows) {
+                const int from = index[i];
+                if (from > i && from < a.c.row_slots) {
+                    src = slot_row(a.c, r, from);
+                    dst = slot_row(a.c, r, i);
+                }
+            }
+            s_src[side][tid] = src < 0 || dst < 0 ? 0 : src + h;   // one that stays reads the first row
+            s_dst[side][tid] = src < 0 || dst < 0 ? -1 : dst + h;
+        }
+    };
+    auto load = [&](int side, Held& v) {
+#pragma unroll
+        for (int k = 0; k < kHold; ++k) {
+            const int row = min(set, sets - 1) + k * sets;
+            const int64_t src = s_src[side][row];
+            v.to[k] = mine ? s_dst[side][row] : -1;
+            v.x[k] = *reinterpret_cast<const piece_t*>(base + src * a.c.row_bytes + at);
+            v.s[k] = scales ? scales[src] : 0.0f;
+        }
+    };
+    auto store = [&](const Held& v) {
+#pragma unroll
+        for (int k = 0; k < kHold; ++k)
+            if (v.to[k] >= 0) {
+                *reinterpret_cast<piece_t*>(base + v.to[k] * a.c.row_bytes + at) = v.x[k];
+                if (scales && piece == 0) scales[v.to[k]] = v.s[k];
+            }
+    };
+    Held now, next;
+    look_up(0, 0);
+    look_up(group, 1);
+    __syncthreads();
+    load(0, now);
+    int side = 1;
+    for (int i0 = 0; i0 < rows; i0 += group, side ^= 1) {
+        arrived(now);
+        __syncthreads();                         // all of this group is in registers
+        load(side, next);
+        // the places of the group after that go where this one's were
+        look_up(i0 + 2 * group, side ^ 1);
+        store(now);
+        now = next;
+    }
+}
+
+// Commit: one workgroup per request and kHold planes; rows of all heads lie side
+// by side, and a lane holds one piece of a row in every plane.
+__global__ void __launch_bounds__(kWg) kvx_commit_kernel(const MoveArgs a)
+{
+    __shared__ int64_t s_src[kWg], s_dst[kWg];
+    const int tid = int(threadIdx.x), lane = tid & 63, R = a.c.num_requests;
+    const int r = int(blockIdx.x) % R, plane0 = int(blockIdx.x) / R * kHold;
+    const int planes = min(kHold, 2 * a.num_layers - plane0);
+    // the path's length: entries ascend strictly and their slots lie in the row
+    const int first = max(a.contexts[r], 0);
+    const int32_t* const index = a.index + int64_t(r) * a.stride;
+    const int most = min(a.counts[r], a.stride);
+    int rows = 0;
+    while (rows < most) {
+        const int i = rows + lane;
+        const int e = i < most ? index[i] : 0, before = i > 0 && i < most ? index[i - 1] : -1;
+        const uint64_t good = __ballot(i < most && e > before && int64_t(first) + e < a.c.row_slots);
+        if (good != ~uint64_t(0)) {
+            rows += __builtin_ctzll(~good);
+            break;
+        }
+        rows += 64;
+    }
+    if (plane0 == 0 && tid == 0) a.new_lens[r] = first + rows;
+    if (planes <= 0) return;
+    char* const base = a.c.base + plane0 * a.c.plane_bytes;
+    float* const scales = a.c.scales ? a.c.scales + plane0 * a.c.plane_scales : nullptr;
+    const int pieces = a.c.hd * a.c.row_bytes >> 4, lg = a.lg_lanes;
+    const int per = 1 << lg, sets = kWg >> lg, set = tid >> lg, piece0 = tid & (per - 1);
+    for (int i0 = 0; i0 < rows; i0 += kWg) {
+        __syncthreads();                         // the last ones' places are read
+        if (i0 + tid < rows) {
+            const int i = i0 + tid, from = index[i];
+            int64_t src = -1, dst = -1;
+            if (from > i) {
                 src = slot_row(a.c, r, first + from);
                 dst = slot_row(a.c, r, first + i);
             }
-            if (src < 0) dst = -1;
+            s_src[tid] = src < 0 || dst < 0 ? 0 : src;
+            s_dst[tid] = src < 0 || dst < 0 ? -1 : dst;
         }
-        if (dst >= 0) {
-            x = *reinterpret_cast<const uint4*>(base + (src + h) * a.c.row_bytes + piece * 16);
-            if (scales && piece == 0) s = scales[src + h];
-        }
-        __builtin_amdgcn_s_waitcnt(0);                     // this group's rows are in registers
         __syncthreads();
-        if (dst >= 0) {
-            *reinterpret_cast<uint4*>(base + (dst + h) * a.c.row_bytes + piece * 16) = x;
-            if (scales && piece == 0) scales[dst + h] = s;
+        const int end = min(rows - i0, kWg);
+        for (int row0 = 0; row0 < end; row0 += sets) {
+            const int row = min(row0 + set, end - 1);
+            const int64_t src = s_src[row], dst = row0 + set < end ? s_dst[row] : -1;
+            for (int turn = 0; turn < pieces; turn += per) {
+                const int piece = turn + piece0, part = min(piece, pieces - 1), head = min(piece, a.c.hd - 1);
+                Held v;
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) {
+                    const int64_t p = min(k, planes - 1);
+                    v.x[k] = *reinterpret_cast<const piece_t*>(base + p * a.c.plane_bytes +
+                                                               src * a.c.row_bytes + part * 16);
+                    v.s[k] = scales ? scales[p * a.c.plane_scales + src + head] : 0.0f;
+                }
+                arrived(v);
+                __syncthreads();
+#pragma unroll
+                for (int k = 0; k < kHold; ++k)
+                    if (k < planes && dst >= 0) {
+                        if (piece < pieces)
+                            *reinterpret_cast<piece_t*>(base + k * a.c.plane_bytes + dst * a.c.row_bytes + piece * 16) = v.x[k];
+                        if (scales && piece < a.c.hd) scales[k * a.c.plane_scales + dst + piece] = v.s[k];
+                    }
+            }
         }
     }
 }
-
-// The accepted paths' lengths: entries ascend strictly and their slots lie in
-// the block-table row; the first that does not ends the path.
-__global__ void __launch_bounds__(kWg) kvx_path_kernel(const CacheArgs c, const CommitArgs a)
-{
-    const int r = int(blockIdx.x) * kWg + int(threadIdx.x);
-    if (r >= c.num_requests) return;
-    const int first = max(a.contexts[r], 0);
-    const int most = min(a.counts[r], a.a_stride);
-    int n = 0, before = -1;
-    while (n < most) {
-        const int e = a.accepted[int64_t(r) * a.a_stride + n];
-        if (e <= before || int64_t(first) + e >= c.row_slots) break;
-        before = e;
-        ++n;
-    }
-    a.new_lens[r] = first + n;
-}
-
-int done() { return int(hipGetLastError()); }
 
 template <typename K, typename A>
-int run(K kernel, int64_t grid, const A& args, void* stream)
+int run(K kernel, int64_t grid, int threads, const A& args, void* stream)
 {
-    kernel<<<dim3(uint32_t(grid)), dim3(kWg), 0, static_cast<hipStream_t>(stream)>>>(args);
-    return done();
+    kernel<<<dim3(uint32_t(grid)), dim3(threads), 0, static_cast<hipStream_t>(stream)>>>(args);
+    return int(hipGetLastError());
+}
+
+template <bool kBf16, int kCache, int kPairing>
+int append_by(const AppendArgs& a, void* stream)
+{
+    // four tokens share a workgroup's start where there are workgroups enough for the card
+    const int64_t n = a.b.total_tokens;
+    return n >= 2048 ? run(kvx_append_kernel<kBf16, kCache, kPairing, 4>, (n + 3) / 4, kWg, a, stream)
+                     : run(kvx_append_kernel<kBf16, kCache, kPairing, 1>, n, kWg, a, stream);
+}
+
+template <bool kBf16, int kCache>
+int append_to(const AppendArgs& a, void* stream)
+{
+    if (a.interleaved) return append_by<kBf16, kCache, kInterleaved>(a, stream);
+    return a.pairs % 8 ? append_by<kBf16, kCache, kAnyHalves>(a, stream)
+                       : append_by<kBf16, kCache, kHalves>(a, stream);
 }
 
 template <bool kBf16>
 int append_as(const AppendArgs& a, int cache_dtype, void* stream)
 {
-    const int64_t n = a.b.total_tokens;
     switch (cache_dtype) {
-    case KVX_FP16: return run(kvx_append_kernel<kBf16, KVX_FP16>, n, a, stream);
-    case KVX_BF16: return run(kvx_append_kernel<kBf16, KVX_BF16>, n, a, stream);
-    case KVX_FP8_E4M3FN: return run(kvx_append_kernel<kBf16, KVX_FP8_E4M3FN>, n, a, stream);
-    default: return run(kvx_append_kernel<kBf16, KVX_FP8_E5M2>, n, a, stream);
+    case KVX_FP16: return append_to<kBf16, KVX_FP16>(a, stream);
+    case KVX_BF16: return append_to<kBf16, KVX_BF16>(a, stream);
+    case KVX_FP8_E4M3FN: return append_to<kBf16, KVX_FP8_E4M3FN>(a, stream);
+    default: return append_to<kBf16, KVX_FP8_E5M2>(a, stream);
     }
+}
+
+// lanes of a row of `bytes`: 16 bytes each, a power of two, at most a workgroup's
+int row_lanes(int64_t bytes)
+{
+    int lg = 0;
+    while (lg < 8 && (int64_t(16) << lg) < bytes) ++lg;
+    return lg;
 }
 
 }  // namespace
@@ -351,32 +537,35 @@ int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream)
 int launch_evict(const EvictArgs& a, int num_layers, void* stream)
 {
     const int64_t units = int64_t(num_layers) * a.c.num_requests * a.c.hd;
-    const int err = run(kvx_select_kernel, units, a, stream);
+    // long requests take more threads: the passes over the weights are a chain
+    const int err = a.max_len > 4096 ? run(kvx_select_kernel<1024>, units, 1024, a, stream)
+                                     : run(kvx_select_kernel<256>, units, 256, a, stream);
     if (err) return err;
     MoveArgs m = {};
     m.c = a.c;
     m.index = a.kept;
     m.stride = a.budget;
     m.num_layers = num_layers;
+    m.lg_lanes = row_lanes(a.c.row_bytes);
     m.lens = a.lens;
     m.max_len = a.max_len;
-    return run(kvx_move_kernel<false>, 2 * units, m, stream);
+    return run(kvx_move_kernel, 2 * units, kWg, m, stream);
 }
 
 int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void* stream)
 {
-    kvx_path_kernel<<<dim3((c.num_requests + kWg - 1) / kWg), dim3(kWg), 0,
-                      static_cast<hipStream_t>(stream)>>>(c, a);
-    const int err = done();
-    if (err || num_layers == 0 || a.a_stride == 0) return err;
     MoveArgs m = {};
     m.c = c;
     m.index = a.accepted;
     m.stride = a.a_stride;
     m.num_layers = num_layers;
+    m.lg_lanes = row_lanes(int64_t(c.hd) * c.row_bytes);
     m.contexts = a.contexts;
+    m.counts = a.counts;
     m.new_lens = a.new_lens;
-    return run(kvx_move_kernel<true>, int64_t(2) * num_layers * c.num_requests * c.hd, m, stream);
+    // at least one plane's workgroups, which write new_lens
+    const int64_t groups = std::max<int64_t>(1, (2 * int64_t(num_layers) + kHold - 1) / kHold);
+    return run(kvx_commit_kernel, groups * c.num_requests, kWg, m, stream);
 }
 
 }  // namespace kvx

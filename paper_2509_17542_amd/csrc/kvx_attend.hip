@@ -131,8 +131,9 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
 {
     AttendPlan p = {};
     p.rows = int(std::min<int64_t>(int64_t(b.max_tokens) * (q_heads / c.num_kv_heads), INT32_MAX));
-    p.few = p.rows <= 32;
-    p.tile_rows = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
+    // 17 to 32 rows of more than 128 elements do not fit the few-rows kernel's registers
+    p.few = p.rows <= (c.head_dim > 128 ? 16 : 32);
+    p.tile_rows = p.few ? (p.rows <= 16 ? 16 : 32) : p.rows <= 64 ? 64 : 128;
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     if (p.few) {
         p.chunk = 512;

@@ -31,20 +31,22 @@ struct Words {
     uint32_t w[kBytes / 4];
 };
 
+// Rows that are read once: non-temporal (a stream of 256-byte pieces at strides of
+// 2 KB reads at 6.5 TB/s so, at 5.8 without).
 template <int kBytes>
 __device__ __forceinline__ Words<kBytes> load_words(const char* p)
 {
+    constexpr int kN = kBytes / 4 < 4 ? kBytes / 4 : 4;
+    typedef uint32_t part_t __attribute__((ext_vector_type(kN)));
     Words<kBytes> v;
-    if constexpr (kBytes == 4) {
-        v.w[0] = *reinterpret_cast<const uint32_t*>(p);
-    } else if constexpr (kBytes == 8) {
-        const uint2 x = *reinterpret_cast<const uint2*>(p);
-        v.w[0] = x.x, v.w[1] = x.y;
-    } else {
 #pragma unroll
-        for (int i = 0; i < kBytes / 16; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p + 16 * i);
-            v.w[4 * i] = x.x, v.w[4 * i + 1] = x.y, v.w[4 * i + 2] = x.z, v.w[4 * i + 3] = x.w;
+    for (int i = 0; i < kBytes / 4 / kN; ++i) {
+        const part_t x = __builtin_nontemporal_load(reinterpret_cast<const part_t*>(p) + i);
+        if constexpr (kN == 1) {
+            v.w[0] = __builtin_bit_cast(uint32_t, x);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kN; ++k) v.w[kN * i + k] = x[k];
         }
     }
     return v;
@@ -59,25 +61,32 @@ __device__ __forceinline__ Words<kBytes> no_words()
     return v;
 }
 
-// One tile's K and V as a lane holds them.
+// One wave's tile: K as it is read, V as the matrix instructions take it.
 template <int kCodes, int DP>
 struct Tile {
     static constexpr int kEl = kCodes == kCodes16 ? 2 : 1;
     static constexpr int DT = DP / 16;
     static constexpr int kVBytes = DT * kEl;
-    // K: pieces of 16 bytes, 8 elements or 16 codes
-    static constexpr int kPieces = DP * kEl / 64;
-    Words<16> k[2][kPieces];
+    static constexpr int kRow = DP * kEl;           // bytes of a row
+    static constexpr int kPieces = kRow / 16;       // 16-byte pieces of it, 8 elements or 16 codes
+    static constexpr int kLoads = kTile * kRow / 1024;
+    // Piece p of slot s lies at place p ^ turn_of(s) of the slot's row in LDS: 16 slots' pieces
+    // of one number, which the matrix instructions take together, then lie in different banks.
+    __device__ static __forceinline__ int turn_of(int s)
+    {
+        return kRow >= 256 ? s & 15 : (s / (256 / kRow)) & (kPieces - 1);
+    }
+    Words<16> k[kLoads];
     Words<kVBytes> v[8];
 };
 
 // Registers decide how many waves a SIMD holds: O takes DP RT / 4, K and V up to
 // DP / 4 each.
-template <int DP, int RT>
-constexpr int kWavesPerSimd = DP >= 256 ? 1 : DP * RT >= 128 ? 2 : 3;
+template <int kCodes, int DP, int RT>
+constexpr int kWavesPerSimd = DP >= 256 ? 1 : DP * RT >= 256 || (DP >= 128 && kCodes == kCodes16) ? 2 : 3;
 
 template <bool kBf16, int kCodes, int DP, int RT, bool kGeneral>
-__global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_kernel(const AttendArgs a)
+__global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_attend_few_kernel(const AttendArgs a)
 {
     using T = Tile<kCodes, DP>;
     constexpr int DT = T::DT, kRows = 16 * RT;
@@ -86,6 +95,8 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
     constexpr int kKeyBytes = kMaxChunk * (k8 ? 20 : 12);
     constexpr int kSlabBytes = 2 * kRows * DP * 4;
     __shared__ __attribute__((aligned(16))) char smem[kKeyBytes > kSlabBytes ? kKeyBytes : kSlabBytes];
+    __shared__ __attribute__((aligned(16))) char s_k[kWaves][kTile * T::kRow];
+    __shared__ uint64_t s_valid[kMaxChunk / 64];
     __shared__ float s_ml[kWaves][kRows][2];
     int64_t* const s_off = reinterpret_cast<int64_t*>(smem);
     int32_t* const s_pos = reinterpret_cast<int32_t*>(smem + kMaxChunk * 8);
@@ -116,10 +127,12 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
     }
 
     // places of the chunk's slots
-    for (int v = v0 + tid; v < v0 + a.chunk && v < v1 + kTile; v += kWg) {
-        const int j = rg.slot(v);
+    for (int base = v0; base < v1; base += kWg) {
+        const int v = base + tid, j = rg.slot(v);
         const int64_t row = v < v1 && j < rq.total ? slot_row(a.c, r, j) : -1;
-        s_off[v - v0] = row < 0 ? -1 : (row + h) * a.c.row_bytes;
+        const uint64_t some = __ballot(row >= 0);
+        if (lane == 0) s_valid[(v - v0) >> 6] = some;
+        s_off[v - v0] = row < 0 ? 0 : (row + h) * a.c.row_bytes;
         s_pos[v - v0] = a.b.positions && j >= rq.ctx && j < rq.total ? a.b.positions[rq.first + j - rq.ctx] : j;
         if constexpr (k8) {
             s_ks[v - v0] = row < 0 ? 0.0f : a.c.scales[row + h];
@@ -167,27 +180,34 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
     // Loads take no branch: a slot that lies in no page reads the plane's first
     // row, a lane past the row's end its first piece.  What comes of the former is
     // masked (turn), of the latter multiplied by q's zeros or not written.
-    int k_at[T::kPieces];
-#pragma unroll
-    for (int p = 0; p < T::kPieces; ++p) {
-        const int at = p * 64 + g * 16;
-        k_at[p] = at < a.c.row_bytes ? at : 0;
-    }
     const int v_at = n16 * T::kVBytes < a.c.row_bytes ? n16 * T::kVBytes : 0;
     const int v_more = v_at + 16 < a.c.row_bytes ? v_at + 16 : 0;   // the second piece of 32 bytes
 
-    auto load_k = [&](int v, T& x) {   // slot n16 of each half, 16-byte pieces g, g + 4, ...
+    // K: whole rows, 1 KB an instruction
+    auto load_k = [&](int v, T& x) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const char* const row = kb + max(s_off[v - v0 + 16 * s + n16], int64_t(0));
-#pragma unroll
-            for (int p = 0; p < T::kPieces; ++p) x.k[s][p] = load_words<16>(row + k_at[p]);
+        for (int i = 0; i < T::kLoads; ++i) {
+            const int s = (i * 64 + lane) / T::kPieces, piece = (i * 64 + lane) % T::kPieces * 16;
+            x.k[i] = load_words<16>(kb + s_off[v - v0 + s] + (piece < a.c.row_bytes ? piece : 0));
         }
+    };
+    auto put_k = [&](const T& x) {
+#pragma unroll
+        for (int i = 0; i < T::kLoads; ++i) {
+            const int s = (i * 64 + lane) / T::kPieces, place = ((i * 64 + lane) % T::kPieces) ^ T::turn_of(s);
+            *reinterpret_cast<u32x4*>(s_k[wave] + s * T::kRow + place * 16) =
+                u32x4{x.k[i].w[0], x.k[i].w[1], x.k[i].w[2], x.k[i].w[3]};
+        }
+    };
+    // piece p of slot n16 of a half
+    auto k_piece = [&](int half, int p) {
+        const int s = 16 * half + n16;
+        return *reinterpret_cast<const u32x4*>(s_k[wave] + s * T::kRow + ((p ^ T::turn_of(s)) << 4));
     };
     auto load_v = [&](int v, T& x) {   // slots 4 g .. 4 g + 3 of each half, elements n16 DT ..
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const char* const row = vb + max(s_off[v - v0 + 16 * (j >> 2) + 4 * g + (j & 3)], int64_t(0));
+            const char* const row = vb + s_off[v - v0 + 16 * (j >> 2) + 4 * g + (j & 3)];
             if constexpr (T::kVBytes == 32) {
                 const Words<16> y = load_words<16>(row + v_at), z = load_words<16>(row + v_more);
 #pragma unroll
@@ -217,8 +237,8 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
 
     // the tile's slots that lie in a page
     auto valid_of = [&](int v) {
-        const uint64_t b0 = __ballot(s_off[v - v0 + n16] >= 0), b1 = __ballot(s_off[v - v0 + 16 + n16] >= 0);
-        return uint32_t(b0 & 0xFFFFu) | uint32_t(b1 & 0xFFFFu) << 16;
+        return uint32_t(__builtin_amdgcn_readfirstlane(
+            int(uint32_t(s_valid[(v - v0) >> 6] >> ((v - v0) & 32)))));
     };
     // whether every row sees the tile whole
     auto is_whole = [&](int v, uint32_t valid) {
@@ -267,6 +287,8 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
             const uint32_t e = (__float_as_uint(fresh_ref) + 0x7FFFFFu) & 0x7F800000u;
             fresh_ref = __uint_as_float(min(max(e, 0x00800000u), 0x7E800000u));
         }
+        put_k(x);
+        load_k(next, x);               // the next turn's keys take their place
         f32x4 s[RT][2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -276,17 +298,15 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<DP, RT>)) kvx_attend_few_k
             for (int c = 0; c < DP / 32; ++c) {
                 u32x4 f;
                 if constexpr (k8) {
-                    const Words<16>& w = x.k[e][c >> 1];
-                    f = widen8<kBf16, kCodes>(w.w[2 * (c & 1)], w.w[2 * (c & 1) + 1]);
+                    const u32x4 w = k_piece(e, 4 * (c >> 1) + g);
+                    f = c & 1 ? widen8<kBf16, kCodes>(w.z, w.w) : widen8<kBf16, kCodes>(w.x, w.y);
                 } else {
-                    const Words<16>& w = x.k[e][c];
-                    f = u32x4{w.w[0], w.w[1], w.w[2], w.w[3]};
+                    f = k_piece(e, 4 * c + g);
                 }
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) s[rt][e] = mfma16<kBf16>(f, q[rt][c], s[rt][e]);
             }
         }
-        load_k(next, x);               // the next turn's keys take their place
         u32x4 pf[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -515,7 +535,7 @@ int pick(const AttendArgs& a, const AttendPlan& p, void* stream)
     const bool two = p.tile_rows > 16;
     if (a.c.dim <= 64) return two ? go<kBf16, kCodes, 64, 2>(a, stream) : go<kBf16, kCodes, 64, 1>(a, stream);
     if (a.c.dim <= 128) return two ? go<kBf16, kCodes, 128, 2>(a, stream) : go<kBf16, kCodes, 128, 1>(a, stream);
-    return two ? go<kBf16, kCodes, 256, 2>(a, stream) : go<kBf16, kCodes, 256, 1>(a, stream);
+    return go<kBf16, kCodes, 256, 1>(a, stream);
 }
 
 }  // namespace

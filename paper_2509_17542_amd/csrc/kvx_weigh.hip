@@ -23,6 +23,8 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
 {
     constexpr bool k8 = kCodes != kCodes16;
     constexpr int kEl = k8 ? 1 : 2, kPieces = DP * kEl / 64, NC = DP / 32;
+    constexpr int kRow = DP * kEl, kRowPieces = kRow / 16, kLoads = 32 * kRow / 1024;
+    __shared__ __attribute__((aligned(16))) char s_k[kWaves][32 * kRow];
     __shared__ int64_t s_off[kWaves][kKeys];
     __shared__ int32_t s_pos[kWaves][kKeys];
     __shared__ float s_ks[kWaves][kKeys];
@@ -52,22 +54,72 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
     const uint64_t valid = __ballot(s_off[wave][lane] >= 0);
     const bool whole = j0 >= rg.all_lo && j0 + kKeys <= rg.all_hi && valid == ~uint64_t(0);
 
-    // keys: slot 16 e + n16, in the element order of 16-byte pieces g, g + 4, ...
+    // Query rows: a lane takes row n16 of 16; the next 16 are on their way while these pass.
+    struct Rows {
+        u32x4 q[NC];
+        float lse;
+        int tok, head, qpos;
+        bool live;
+    };
+    auto read_rows = [&](int row0, Rows& x) {
+        const int row = row0 + n16;
+        x.live = row < rows;
+        const int rr = x.live ? row : 0;
+        x.tok = int(fast_div(uint32_t(rr), a.div_group));
+        x.head = h * G + (rr - x.tok * G);
+        const int64_t token = rq.first + x.tok;
+        const uint16_t* const src = a.q + token * a.q_stride + int64_t(x.head) * D;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int d = k8 ? (c >> 1) * 64 + g * 16 + (c & 1) * 8 : c * 32 + g * 8;
+            x.q[c] = *reinterpret_cast<const u32x4*>(src + (d < D ? d : 0));
+            if (d >= D) x.q[c] = u32x4{0, 0, 0, 0};
+        }
+        x.lse = a.lse[token * a.q_heads + x.head];
+        x.qpos = a.b.positions ? a.b.positions[token] : rq.ctx + x.tok;
+    };
+    // lane (n16, g) writes slot 16 (n16 / 4) + 4 g + n16 % 4
+    const int j = j0 + 16 * (n16 >> 2) + 4 * g + (n16 & 3);
+    float* const out = a.weights + (int64_t(r) * a.c.hd + h) * a.w_stride + min(j, rq.total - 1);
+    const float old = *out;
+    Rows now;
+    read_rows(0, now);
+
+    // Keys: slot 16 e + n16, in the element order of 16-byte pieces g, g + 4, ...  Rows are
+    // read whole, 1 KB an instruction, and turned round in LDS of the wave's own, 32 slots
+    // at a time; piece p of slot s lies at place p ^ turn_of(s), so that 16 slots' pieces
+    // of one number lie in different banks.
+    auto turn_of = [](int s) { return kRow >= 256 ? s & 15 : (s / (256 / kRow)) & (kRowPieces - 1); };
+    u32x4 raw[2][kLoads];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int s = (i * 64 + lane) / kRowPieces, piece = (i * 64 + lane) % kRowPieces * 16;
+            raw[half][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+                a.c.base + max(s_off[wave][32 * half + s], int64_t(0)) + (piece < a.c.row_bytes ? piece : 0)));
+        }
     u32x4 k[4][NC];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const char* const row = a.c.base + max(s_off[wave][16 * e + n16], int64_t(0));
+    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const int at = p * 64 + g * 16;
-            const u32x4 w = *reinterpret_cast<const u32x4*>(row + (at < a.c.row_bytes ? at : 0));
-            if constexpr (k8) {
-                k[e][2 * p] = widen8<kBf16, kCodes>(w.x, w.y);
-                k[e][2 * p + 1] = widen8<kBf16, kCodes>(w.z, w.w);
-            } else {
-                k[e][p] = w;
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            const int s = (i * 64 + lane) / kRowPieces, place = ((i * 64 + lane) % kRowPieces) ^ turn_of(s);
+            *reinterpret_cast<u32x4*>(s_k[wave] + s * kRow + place * 16) = raw[half][i];
         }
+#pragma unroll
+        for (int e = 2 * half; e < 2 * half + 2; ++e)
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                const int s = 16 * (e & 1) + n16;
+                const u32x4 w = *reinterpret_cast<const u32x4*>(s_k[wave] + s * kRow + ((4 * p + g) ^ turn_of(s)) * 16);
+                if constexpr (k8) {
+                    k[e][2 * p] = widen8<kBf16, kCodes>(w.x, w.y);
+                    k[e][2 * p + 1] = widen8<kBf16, kCodes>(w.z, w.w);
+                } else {
+                    k[e][p] = w;
+                }
+            }
     }
     float ks[4][4], acc[4][4];
 #pragma unroll
@@ -80,25 +132,12 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
     const ScoreArgs sc = score_args(a);
 
     for (int row0 = 0; row0 < rows; row0 += 16) {
-        const int row = row0 + n16;
-        const bool live = row < rows;
-        const int rr = live ? row : row0;
-        const int tok = int(fast_div(uint32_t(rr), a.div_group)), head = h * G + (rr - tok * G);
-        const int64_t token = rq.first + tok;
-        const uint16_t* const src = a.q + token * a.q_stride + int64_t(head) * D;
-        u32x4 q[NC];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int d = k8 ? (c >> 1) * 64 + g * 16 + (c & 1) * 8 : c * 32 + g * 8;
-            q[c] = u32x4{0, 0, 0, 0};
-            if (d < D) q[c] = *reinterpret_cast<const u32x4*>(src + d);
-        }
-        const float lse = a.lse[token * a.q_heads + head];
-        const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
-        const int qpos = a.b.positions ? a.b.positions[token] : rq.ctx + tok;
-        const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
-        uint64_t mine = live && lse != -INFINITY ? ~uint64_t(0) : 0;
-        if (!whole && mine) mine = seen_of(a, rq, r, tok, qpos, j0, valid);
+        Rows next;
+        read_rows(row0 + 16 < rows ? row0 + 16 : row0, next);
+        const float lse2 = now.lse == -INFINITY ? INFINITY : now.lse * kLog2e;
+        const float slope2 = a.slopes ? a.slopes[now.head] * kLog2e : 0.0f;
+        uint64_t mine = now.live && now.lse != -INFINITY ? ~uint64_t(0) : 0;
+        if (!whole && mine) mine = seen_of(a, rq, r, now.tok, now.qpos, j0, valid);
         mine >>= 4 * g;
         constexpr uint64_t kOwn = 0x000F000F000F000Full;
         const bool all = __all((mine & kOwn) == kOwn);
@@ -106,16 +145,17 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
         for (int e = 0; e < 4; ++e) {
             f32x4 s = {0, 0, 0, 0};
 #pragma unroll
-            for (int c = 0; c < NC; ++c) s = mfma16<kBf16>(k[e][c], q[c], s);
+            for (int c = 0; c < NC; ++c) s = mfma16<kBf16>(k[e][c], now.q[c], s);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float dot = k8 ? s[i] * ks[e][i] : s[i];
-                const float x = sc.general ? general_score(sc, dot, slope2, qpos - s_pos[wave][16 * e + 4 * g + i])
+                const float x = sc.general ? general_score(sc, dot, slope2, now.qpos - s_pos[wave][16 * e + 4 * g + i])
                                            : dot * sc.c2;
                 const float p = __builtin_amdgcn_exp2f(x - lse2);
                 acc[e][i] += all || (mine >> (16 * e + i) & 1) ? p : 0.0f;
             }
         }
+        now = next;
     }
     // the rows' sums: over the 16 lanes of a group
 #pragma unroll
@@ -129,18 +169,13 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
             x += __shfl_xor(x, 8);
             acc[e][i] = x;
         }
-    // lane (n16, g) writes slot 16 (n16 / 4) + 4 g + n16 % 4
     float w = 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (n16 == 4 * e + i) w = acc[e][i];
-    const int j = j0 + 16 * (n16 >> 2) + 4 * g + (n16 & 3);
-    if (j < rq.total) {
-        float* const out = a.weights + (int64_t(r) * a.c.hd + h) * a.w_stride + j;
-        *out = j < rq.ctx ? *out + w : w;
-    }
+    if (j < rq.total) *out = j < rq.ctx ? old + w : w;
 }
 
 template <bool kBf16, int kCodes, int DP>

@@ -177,24 +177,27 @@ def make_rope(inv_freq, sections, positions, interleaved=False) -> kvx_rope:
     return r
 
 
-def _rows(x, what, tokens, dim, dtype=None):
-    """A [tokens][heads][dim] device tensor whose heads are contiguous: its token
-    stride in elements."""
-    if x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != dim:
+def _rows(x, what, tokens, dim, dtype):
+    """A [tokens][heads][dim] device tensor whose heads are contiguous: its heads
+    and the elements between tokens.  dtype None: float16 or bfloat16."""
+    try:
+        n, heads, d = x.shape
+        s0, s1, s2 = x.stride()
+    except ValueError:
+        raise ValueError(f"{what} must be [{tokens}][heads][{dim}], not {list(x.shape)}") from None
+    if n == tokens and d == dim and x.is_cuda and (s1 == dim or heads == 1) and s2 == 1 and \
+            (x.dtype == dtype if dtype is not None else x.dtype in _ROW_TYPES):
+        # one token, or none: no stride between tokens to speak of
+        return heads, s0 if n > 1 else heads * dim
+    if n != tokens or d != dim:
         raise ValueError(f"{what} must be [{tokens}][heads][{dim}], not {list(x.shape)}")
     if not x.is_cuda:
         raise ValueError(f"{what} must be a device tensor, not one on {x.device}")
     if x.dtype not in _ROW_TYPES or (dtype is not None and x.dtype != dtype):
         raise ValueError(f"{what} must be {dtype or 'float16 or bfloat16'}, not {x.dtype}")
-    width = x.shape[1] * dim
-    if tokens == 0 or width == 0:
-        return width + -width % 8
-    s0, s1, s2 = x.stride()
-    if (dim > 1 and s2 != 1) or (x.shape[1] > 1 and s1 != dim):
-        raise ValueError(f"{what}: the heads of a token must be contiguous")
-    if tokens == 1:
-        return width + -width % 8
-    return s0
+    if n * heads == 0:
+        return heads, heads * dim
+    raise ValueError(f"{what}: the heads of a token must be contiguous")
 
 
 def _match(view, batch, scores=None, q_heads=0):
@@ -212,20 +215,21 @@ def kvx_append(view, batch, rope, layer, q, k, v, q_out, stream=None) -> None:
     only), k, v [tokens][Hd][D]; slices of a fused projection serve."""
     _match(view, batch)
     n, d, heads = batch.tokens, view.head_dim, view.num_kv_heads
-    if rope.tokens < n:
+    if rope.tokens != n:
         raise ValueError(f"positions of {rope.tokens} tokens, a batch of {n}")
-    if rope.keep[1].shape[1] != n:
-        raise ValueError(f"positions must be [axes][{n}]")
-    ks, vs = _rows(k, "k", n, d), _rows(v, "v", n, d, k.dtype)
-    if k.shape[1] != heads or v.shape[1] != heads:
+    dtype = k.dtype
+    (k_heads, ks), (v_heads, vs) = _rows(k, "k", n, d, None), _rows(v, "v", n, d, dtype)
+    if k_heads != heads or v_heads != heads:
         raise ValueError(f"k and v must have the cache's {heads} heads")
-    q_heads = qs = os = 0
+    q_heads = qs = out_heads = os = 0
     if q is not None:
-        if q_out is None or q_out.shape != q.shape:
-            raise ValueError("q_out must have the shape of q")
-        q_heads = q.shape[1]
-        qs, os = _rows(q, "q", n, d, k.dtype), _rows(q_out, "q_out", n, d, k.dtype)
-    status = _lib.kvx_append(view.ref, batch.ref, rope.ref, layer, _ROW_TYPES[k.dtype], q_heads,
+        q_heads, qs = _rows(q, "q", n, d, dtype)
+        if q_out is None:
+            raise ValueError("q_out must be given with q")
+        out_heads, os = _rows(q_out, "q_out", n, d, dtype)
+    if q_heads != out_heads:
+        raise ValueError("q_out must have the heads of q")
+    status = _lib.kvx_append(view.ref, batch.ref, rope.ref, layer, _ROW_TYPES[dtype], q_heads,
                              _addr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, _addr(q_out), os,
                              _stream(stream))
     if status:
@@ -243,9 +247,9 @@ def kvx_attend(view, batch, scores, layer, q, out, lse=None, workspace=None, str
     """q, out [tokens][q_heads][D]; lse float32 [tokens][q_heads] or None;
     workspace: a device tensor of kvx_attend_workspace bytes, or None for 0."""
     n, d = batch.tokens, view.head_dim
-    qs, os = _rows(q, "q", n, d), _rows(out, "out", n, d, q.dtype)
-    q_heads = q.shape[1]
-    if out.shape[1] != q_heads:
+    dtype = q.dtype
+    (q_heads, qs), (out_heads, os) = _rows(q, "q", n, d, None), _rows(out, "out", n, d, dtype)
+    if out_heads != q_heads:
         raise ValueError("out must have the heads of q")
     _match(view, batch, scores, q_heads)
     if lse is not None:
@@ -254,7 +258,7 @@ def kvx_attend(view, batch, scores, layer, q, out, lse=None, workspace=None, str
     if workspace is not None:
         nbytes = workspace.nbytes
         _need(workspace, nbytes, "workspace")
-    status = _lib.kvx_attend(view.ref, batch.ref, scores.ref, layer, _ROW_TYPES[q.dtype], q_heads,
+    status = _lib.kvx_attend(view.ref, batch.ref, scores.ref, layer, _ROW_TYPES[dtype], q_heads,
                              q.data_ptr(), qs, out.data_ptr(), os, _addr(lse), _addr(workspace),
                              nbytes, _stream(stream))
     if status:
@@ -265,8 +269,7 @@ def kvx_weigh(view, batch, scores, layer, q, lse, weights, stream=None) -> None:
     """lse float32 [tokens][q_heads] as kvx_attend gave it; weights float32
     [requests][Hd][stride], stride >= the batch's max_context."""
     n, d = batch.tokens, view.head_dim
-    qs = _rows(q, "q", n, d)
-    q_heads = q.shape[1]
+    q_heads, qs = _rows(q, "q", n, d, None)
     _match(view, batch, scores, q_heads)
     _need(lse, 4 * n * q_heads, "lse", torch.float32)
     if weights.dim() != 3 or weights.shape[:2] != (view.num_requests, view.num_kv_heads):

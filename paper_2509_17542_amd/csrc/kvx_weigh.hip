@@ -1,13 +1,17 @@
 // The slots' accumulated attention weight (kvx_weigh).
 //
-// A wave takes 64 slots of one request and KV head: their keys stay in
-// registers as the matrix instructions take them, and the query rows pass by 16
-// at a time,
+// A wave takes 32 or 64 slots of one request and KV head: their rows go to LDS of
+// its own, whole, 32 at a time, and from there to the matrix instructions; the
+// query rows pass by 16 at a time,
 //   S^T = K Q^T,  w[slot] += exp2(x2 - lse2),
 // each lane adding up its own query row's weights; the 16 lanes' sums are added
-// once at the end, in a fixed order.  Bound by reading K for few rows, by the
-// matrix instructions and the exponentials for many.  No two waves write the same
-// slot, so nothing is added atomically.
+// at the end, in a fixed order.  For 16 rows or fewer a wave is a chain (places,
+// rows, products, weights), bound by how many waves a SIMD holds: 32 keys that
+// stay in LDS leave registers for four (32 requests of 512..4096 slots, e5m2: 24
+// us; 30 with 64 keys in registers).  For more it is bound by the matrix
+// instructions and the exponentials, and 64 keys in registers serve all rows
+// (the last 32 tokens of two prompts, 128 rows: 50 us, 68 the other way).  No two
+// waves write the same slot, so nothing is added atomically.
 #include <hip/hip_runtime.h>
 
 #include "kvx_attend_dev.h"
@@ -16,18 +20,21 @@ namespace kvx {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kKeys = 64;                        // slots of a wave
 
-template <bool kBf16, int kCodes, int DP>
-__global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_kernel(const AttendArgs a, int tiles)
+// kHalves: 32 slots each; two are held in registers
+template <bool kBf16, int kCodes, int DP, bool kGeneral, int kHalves>
+__global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : kHalves == 2 ? 3 : 4))
+    kvx_weigh_kernel(const AttendArgs a, int tiles)
 {
+    constexpr int kKeys = 32 * kHalves, kTiles16 = 2 * kHalves;
+    constexpr bool kHeld = kHalves == 2;
     constexpr bool k8 = kCodes != kCodes16;
-    constexpr int kEl = k8 ? 1 : 2, kPieces = DP * kEl / 64, NC = DP / 32;
+    constexpr int kEl = k8 ? 1 : 2, NC = DP / 32;
     constexpr int kRow = DP * kEl, kRowPieces = kRow / 16, kLoads = 32 * kRow / 1024;
     __shared__ __attribute__((aligned(16))) char s_k[kWaves][32 * kRow];
     __shared__ int64_t s_off[kWaves][kKeys];
-    __shared__ int32_t s_pos[kWaves][kKeys];
     __shared__ float s_ks[kWaves][kKeys];
+    __shared__ int32_t s_pos[kWaves][kGeneral ? kKeys : 1];
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4;
     const int D = a.c.dim, G = a.group;
@@ -37,22 +44,35 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
     const int tile = int(u % uint32_t(tiles)), r = int(u / uint32_t(tiles));
     const Request rq = request_of(a.c, a.b, r);
     const int j0 = (tile * kWaves + wave) * kKeys, rows = rq.n * G;
-    const bool some = rows > 0 && j0 < rq.total;
-    {
-        const int j = j0 + lane;
-        const int64_t row = some && j < rq.total ? slot_row(a.c, r, j) : -1;
-        s_off[wave][lane] = row < 0 ? -1 : (row + h) * a.c.row_bytes;
-        s_pos[wave][lane] = a.b.positions && some && j >= rq.ctx && j < rq.total
-                                ? a.b.positions[rq.first + j - rq.ctx] : j;
-        s_ks[wave][lane] = k8 && row >= 0 ? a.c.scales[row + h] : 0.0f;
+    if (rows == 0 || j0 >= rq.total) return;     // waves share nothing
+    const int64_t my_row = lane < kKeys && j0 + lane < rq.total ? slot_row(a.c, r, j0 + lane) : -1;
+    const uint64_t valid = __ballot(my_row >= 0);
+    if (lane < kKeys) {
+        // a slot that lies in no page reads the plane's first row, and is masked
+        s_off[wave][lane] = my_row < 0 ? 0 : (my_row + h) * a.c.row_bytes;
+        if constexpr (k8) s_ks[wave][lane] = my_row < 0 ? 0.0f : a.c.scales[my_row + h];
+        if constexpr (kGeneral) s_pos[wave][lane] = place_of(a, rq, j0 + lane);
     }
-    __syncthreads();
-    if (!some) return;
+    // a wave's LDS is its own and its accesses stay in order: nothing to wait for
+    __builtin_amdgcn_wave_barrier();
     const Range rg = range_of(a, rq, r, 0, rq.n - 1);
-    const bool unseen = a.window > 0 && j0 >= rg.pre && j0 + kKeys <= rg.lo;
-    if (unseen && j0 + kKeys <= rq.ctx) return;
-    const uint64_t valid = __ballot(s_off[wave][lane] >= 0);
-    const bool whole = j0 >= rg.all_lo && j0 + kKeys <= rg.all_hi && valid == ~uint64_t(0);
+    // what no token sees keeps its weight, new tokens' slots apart
+    if (a.window > 0 && j0 >= rg.pre && j0 + kKeys <= rg.lo && j0 + kKeys <= rq.ctx) return;
+    constexpr uint64_t kAll = ~uint64_t(0) >> (64 - kKeys);
+    const bool whole = j0 >= rg.all_lo && j0 + kKeys <= rg.all_hi && valid == kAll;
+
+    // Rows are read whole, 1 KB an instruction; piece p of slot s lies at place
+    // p ^ turn_of(s), so that 16 slots' pieces of one number lie in different banks.
+    auto turn_of = [](int s) { return kRow >= 256 ? s & 15 : (s / (256 / kRow)) & (kRowPieces - 1); };
+    u32x4 raw[kHalves][kLoads];
+#pragma unroll
+    for (int half = 0; half < kHalves; ++half)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int s = (i * 64 + lane) / kRowPieces, piece = (i * 64 + lane) % kRowPieces * 16;
+            raw[half][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+                a.c.base + s_off[wave][32 * half + s] + (piece < a.c.row_bytes ? piece : 0)));
+        }
 
     // Query rows: a lane takes row n16 of 16; the next 16 are on their way while these pass.
     struct Rows {
@@ -78,114 +98,106 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : 3)) kvx_weigh_ke
         x.lse = a.lse[token * a.q_heads + x.head];
         x.qpos = a.b.positions ? a.b.positions[token] : rq.ctx + x.tok;
     };
-    // lane (n16, g) writes slot 16 (n16 / 4) + 4 g + n16 % 4
-    const int j = j0 + 16 * (n16 >> 2) + 4 * g + (n16 & 3);
-    float* const out = a.weights + (int64_t(r) * a.c.hd + h) * a.w_stride + min(j, rq.total - 1);
-    const float old = *out;
     Rows now;
     read_rows(0, now);
-
-    // Keys: slot 16 e + n16, in the element order of 16-byte pieces g, g + 4, ...  Rows are
-    // read whole, 1 KB an instruction, and turned round in LDS of the wave's own, 32 slots
-    // at a time; piece p of slot s lies at place p ^ turn_of(s), so that 16 slots' pieces
-    // of one number lie in different banks.
-    auto turn_of = [](int s) { return kRow >= 256 ? s & 15 : (s / (256 / kRow)) & (kRowPieces - 1); };
-    u32x4 raw[2][kLoads];
+    // of each 16 lanes the first 4 kTiles16 write a slot: 16 (i / 4) + 4 g + i % 4, i being the lane's
+    // bits turned round
+    constexpr int kWriters = 4 * kTiles16, kBits = kHeld ? 4 : 3;
+    const int i16 = int(__builtin_bitreverse32(uint32_t(n16 & (kWriters - 1))) >> (32 - kBits));
+    const int j = j0 + 16 * (i16 >> 2) + 4 * g + (i16 & 3);
+    float* const out = a.weights + (int64_t(r) * a.c.hd + h) * a.w_stride + min(j, rq.total - 1);
+    const float old = *out;
+    const ScoreArgs sc = score_args(a);
+    // the c-th operand of 16 slots of the half that lies in LDS
+    auto operand = [&](int e, int c) {
+        const int slot = 16 * e + n16;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(
+            s_k[wave] + slot * kRow + ((4 * (k8 ? c >> 1 : c) + g) ^ turn_of(slot)) * 16);
+        if constexpr (k8) return c & 1 ? widen8<kBf16, kCodes>(w.z, w.w) : widen8<kBf16, kCodes>(w.x, w.y);
+        return w;
+    };
+    u32x4 held[kHeld ? kTiles16 : 1][NC];
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int s = (i * 64 + lane) / kRowPieces, piece = (i * 64 + lane) % kRowPieces * 16;
-            raw[half][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
-                a.c.base + max(s_off[wave][32 * half + s], int64_t(0)) + (piece < a.c.row_bytes ? piece : 0)));
-        }
-    u32x4 k[4][NC];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    for (int half = 0; half < kHalves; ++half) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int s = (i * 64 + lane) / kRowPieces, place = ((i * 64 + lane) % kRowPieces) ^ turn_of(s);
             *reinterpret_cast<u32x4*>(s_k[wave] + s * kRow + place * 16) = raw[half][i];
         }
+        if constexpr (kHeld) {
 #pragma unroll
-        for (int e = 2 * half; e < 2 * half + 2; ++e)
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int p = 0; p < kPieces; ++p) {
-                const int s = 16 * (e & 1) + n16;
-                const u32x4 w = *reinterpret_cast<const u32x4*>(s_k[wave] + s * kRow + ((4 * p + g) ^ turn_of(s)) * 16);
-                if constexpr (k8) {
-                    k[e][2 * p] = widen8<kBf16, kCodes>(w.x, w.y);
-                    k[e][2 * p + 1] = widen8<kBf16, kCodes>(w.z, w.w);
-                } else {
-                    k[e][p] = w;
-                }
-            }
-    }
-    float ks[4][4], acc[4][4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            ks[e][i] = s_ks[wave][16 * e + 4 * g + i];
-            acc[e][i] = 0.0f;
+                for (int c = 0; c < NC; ++c) held[2 * half + e][c] = operand(e, c);
         }
-    const ScoreArgs sc = score_args(a);
+    }
+    float ks[kTiles16][4], v[4 * kTiles16] = {};
+#pragma unroll
+    for (int e = 0; e < kTiles16; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ks[e][i] = k8 ? s_ks[wave][16 * e + 4 * g + i] * sc.c2 : sc.c2;
 
     for (int row0 = 0; row0 < rows; row0 += 16) {
         Rows next;
-        read_rows(row0 + 16 < rows ? row0 + 16 : row0, next);
+        if (rows > 16) read_rows(row0 + 16 < rows ? row0 + 16 : 0, next);
         const float lse2 = now.lse == -INFINITY ? INFINITY : now.lse * kLog2e;
-        const float slope2 = a.slopes ? a.slopes[now.head] * kLog2e : 0.0f;
+        const float slope2 = kGeneral && a.slopes ? a.slopes[now.head] * kLog2e : 0.0f;
         uint64_t mine = now.live && now.lse != -INFINITY ? ~uint64_t(0) : 0;
         if (!whole && mine) mine = seen_of(a, rq, r, now.tok, now.qpos, j0, valid);
         mine >>= 4 * g;
-        constexpr uint64_t kOwn = 0x000F000F000F000Full;
+        constexpr uint64_t kOwn = 0x000F000F000F000Full & kAll;
         const bool all = __all((mine & kOwn) == kOwn);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < kTiles16; ++e) {
             f32x4 s = {0, 0, 0, 0};
 #pragma unroll
-            for (int c = 0; c < NC; ++c) s = mfma16<kBf16>(k[e][c], now.q[c], s);
+            for (int c = 0; c < NC; ++c) s = mfma16<kBf16>(kHeld ? held[kHeld ? e : 0][c] : operand(e, c), now.q[c], s);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float dot = k8 ? s[i] * ks[e][i] : s[i];
-                const float x = sc.general ? general_score(sc, dot, slope2, now.qpos - s_pos[wave][16 * e + 4 * g + i])
-                                           : dot * sc.c2;
+                float x = s[i] * ks[e][i];
+                if constexpr (kGeneral)
+                    x = general_score(sc, k8 ? s[i] * s_ks[wave][16 * e + 4 * g + i] : s[i], slope2,
+                                      now.qpos - s_pos[wave][16 * e + 4 * g + i]);
                 const float p = __builtin_amdgcn_exp2f(x - lse2);
-                acc[e][i] += all || (mine >> (16 * e + i) & 1) ? p : 0.0f;
+                v[4 * e + i] += all || (mine >> (16 * e + i) & 1) ? p : 0.0f;
             }
         }
-        now = next;
+        if (rows > 16) now = next;
     }
-    // the rows' sums: over the 16 lanes of a group
+    // The rows' sums, over the 16 lanes of a group: in each step a lane gives half of its values
+    // away and adds its partner's to the other half, so that one is left, that of its slot.
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int s = 0; s < kBits; ++s) {
+        const bool upper = n16 >> s & 1;
+        const int half = (kWriters / 2) >> s;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float x = acc[e][i];
-            x += __shfl_xor(x, 1);
-            x += __shfl_xor(x, 2);
-            x += __shfl_xor(x, 4);
-            x += __shfl_xor(x, 8);
-            acc[e][i] = x;
+        for (int i = 0; i < half; ++i) {
+            const float kept = upper ? v[i + half] : v[i], given = upper ? v[i] : v[i + half];
+            v[i] = kept + __shfl_xor(given, 1 << s);
         }
-    float w = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n16 == 4 * e + i) w = acc[e][i];
-    if (j < rq.total) *out = j < rq.ctx ? old + w : w;
+    }
+    const float w = kHeld ? v[0] : v[0] + __shfl_xor(v[0], 8);
+    if (n16 < kWriters && j < rq.total) *out = j < rq.ctx ? old + w : w;
+}
+
+template <bool kBf16, int kCodes, int DP, bool kGeneral, int kHalves>
+int go_as(const AttendArgs& a, void* stream)
+{
+    constexpr int kSlots = kWaves * 32 * kHalves;
+    const int tiles = (a.b.max_context + kSlots - 1) / kSlots;
+    kvx_weigh_kernel<kBf16, kCodes, DP, kGeneral, kHalves>
+        <<<dim3(uint32_t(tiles) * a.c.hd * a.c.num_requests), dim3(64 * kWaves), 0,
+           static_cast<hipStream_t>(stream)>>>(a, tiles);
+    return int(hipGetLastError());
 }
 
 template <bool kBf16, int kCodes, int DP>
 int go(const AttendArgs& a, void* stream)
 {
-    const int tiles = (a.b.max_context + kWaves * kKeys - 1) / (kWaves * kKeys);
-    kvx_weigh_kernel<kBf16, kCodes, DP>
-        <<<dim3(uint32_t(tiles) * a.c.hd * a.c.num_requests), dim3(64 * kWaves), 0,
-           static_cast<hipStream_t>(stream)>>>(a, tiles);
-    return int(hipGetLastError());
+    const bool held = int64_t(a.b.max_tokens) * a.group > 16;
+    if (general_scores(a))
+        return held ? go_as<kBf16, kCodes, DP, true, 2>(a, stream) : go_as<kBf16, kCodes, DP, true, 1>(a, stream);
+    return held ? go_as<kBf16, kCodes, DP, false, 2>(a, stream) : go_as<kBf16, kCodes, DP, false, 1>(a, stream);
 }
 
 template <bool kBf16, int kCodes>

@@ -71,8 +71,8 @@ typedef struct {
     const int32_t *token_starts;/* device [num_requests + 1], non-decreasing, within 0 .. N */
     const int32_t *contexts;    /* device [num_requests] */
     const int32_t *positions;   /* device [N] or NULL: the position of each new token that a bias or
-                                 * a window goes by; NULL: C_r + i for token i of request r.  Slot
-                                 * j < C_r has position j. */
+                                 * a window goes by, within +-2^30; NULL: C_r + i for token i of
+                                 * request r.  Slot j < C_r has position j. */
     const uint64_t *tree;       /* device [N][tree_stride] or NULL: bit j of token i's words says
                                  * whether it sees new token j of its request (itself included).
                                  * NULL: a chain, token i sees tokens 0 .. i. */

@@ -100,9 +100,8 @@ int join_as(const AttendArgs& a, void* stream)
     const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
     int lg_lanes = 0;
     while ((4 << lg_lanes) < a.c.dim) ++lg_lanes;
-    kvx_join_kernel<kBf16, kWaves><<<dim3(uint32_t(kWaves == 4 ? pairs : (pairs + 3) / 4)), dim3(256), 0,
-                                     static_cast<hipStream_t>(stream)>>>(a, lg_lanes);
-    return int(hipGetLastError());
+    return launch_kernel(kvx_join_kernel<kBf16, kWaves>, kWaves == 4 ? pairs : (pairs + 3) / 4, 256, stream, a,
+                         lg_lanes);
 }
 
 int join(const AttendArgs& a, bool bf, void* stream)

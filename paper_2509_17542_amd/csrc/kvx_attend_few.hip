@@ -516,10 +516,8 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
 template <bool kBf16, int kCodes, int DP, int RT, bool kGeneral>
 int go_as(const AttendArgs& a, void* stream)
 {
-    kvx_attend_few_kernel<kBf16, kCodes, DP, RT, kGeneral>
-        <<<dim3(uint32_t(a.c.num_requests) * a.splits * a.c.hd), dim3(kWg), 0,
-           static_cast<hipStream_t>(stream)>>>(a);
-    return int(hipGetLastError());
+    return launch_kernel(kvx_attend_few_kernel<kBf16, kCodes, DP, RT, kGeneral>,
+                         int64_t(a.c.num_requests) * a.splits * a.c.hd, kWg, stream, a);
 }
 
 template <bool kBf16, int kCodes, int DP, int RT>

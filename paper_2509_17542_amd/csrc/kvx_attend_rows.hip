@@ -543,10 +543,8 @@ template <bool kBf16, int kCodes, int DP, int NW, int kScores>
 int go_as(const AttendArgs& a, const AttendPlan& p, void* stream)
 {
     const int64_t groups = int64_t(a.c.num_requests) * a.splits * a.c.hd;
-    kvx_attend_rows_kernel<kBf16, kCodes, DP, NW, kScores>
-        <<<dim3(uint32_t(groups * p.row_tiles)), dim3(64 * NW), 0, static_cast<hipStream_t>(stream)>>>(
-            a, p.row_tiles);
-    return int(hipGetLastError());
+    return launch_kernel(kvx_attend_rows_kernel<kBf16, kCodes, DP, NW, kScores>, groups * p.row_tiles, 64 * NW,
+                         stream, a, p.row_tiles);
 }
 
 template <bool kBf16, int kCodes, int DP, int NW>

@@ -280,8 +280,10 @@ extern "C" kvx_status kvx_attend(const kvx_cache* c, const kvx_batch* b, const k
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return fail(KVX_EINVAL, "a 16-byte aligned workspace of %llu bytes is needed, %llu are given",
                     (unsigned long long)need, (unsigned long long)(workspace ? workspace_bytes : 0));
-    if (int64_t(b->total_tokens) * q_heads > kMaxGrid)
-        return fail(KVX_EUNSUPPORTED, "more than 2^31 - 1 query rows");
+    const kvx::AttendPlan plan = kvx::attend_plan(*c, *b, q_heads);
+    if (int64_t(b->total_tokens) * q_heads > kMaxGrid ||
+        double(c->num_requests) * c->num_kv_heads * plan.splits * plan.row_tiles > double(kMaxGrid))
+        return fail(KVX_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
     KVX_TRY(need_device());
     kvx::AttendArgs a = attend_args(*c, *b, *s, layer, q_heads);
     a.q = static_cast<const uint16_t*>(q);
@@ -289,8 +291,7 @@ extern "C" kvx_status kvx_attend(const kvx_cache* c, const kvx_batch* b, const k
     a.lse = lse;
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    return launched(kvx::launch_attend(a, kvx::attend_plan(*c, *b, q_heads), dtype,
-                                       c->dtype, workspace, stream));
+    return launched(kvx::launch_attend(a, plan, dtype, c->dtype, workspace, stream));
 }
 
 extern "C" kvx_status kvx_weigh(const kvx_cache* c, const kvx_batch* b, const kvx_scores* s,

@@ -4,9 +4,22 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kvx_ops_internal.h"
 
 namespace kvx {
+
+// Enqueues `kernel` and returns this launch's hipError_t (an earlier call's error
+// is not taken for it).
+template <typename... P>
+int launch_kernel(void (*kernel)(P...), int64_t grid, int threads, void* stream,
+                  const std::common_type_t<P>&... p)
+{
+    void* args[] = {const_cast<void*>(static_cast<const void*>(&p))...};
+    return int(hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(uint32_t(grid)),
+                               dim3(uint32_t(threads)), args, 0, static_cast<hipStream_t>(stream)));
+}
 
 __device__ __forceinline__ uint32_t fast_div(uint32_t n, FastDiv d)
 {

@@ -488,20 +488,13 @@ __global__ void __launch_bounds__(kWg) kvx_commit_kernel(const MoveArgs a)
     }
 }
 
-template <typename K, typename A>
-int run(K kernel, int64_t grid, int threads, const A& args, void* stream)
-{
-    kernel<<<dim3(uint32_t(grid)), dim3(threads), 0, static_cast<hipStream_t>(stream)>>>(args);
-    return int(hipGetLastError());
-}
-
 template <bool kBf16, int kCache, int kPairing>
 int append_by(const AppendArgs& a, void* stream)
 {
     // four tokens share a workgroup's start where there are workgroups enough for the card
     const int64_t n = a.b.total_tokens;
-    return n >= 2048 ? run(kvx_append_kernel<kBf16, kCache, kPairing, 4>, (n + 3) / 4, kWg, a, stream)
-                     : run(kvx_append_kernel<kBf16, kCache, kPairing, 1>, n, kWg, a, stream);
+    return n >= 2048 ? launch_kernel(kvx_append_kernel<kBf16, kCache, kPairing, 4>, (n + 3) / 4, kWg, stream, a)
+                     : launch_kernel(kvx_append_kernel<kBf16, kCache, kPairing, 1>, n, kWg, stream, a);
 }
 
 template <bool kBf16, int kCache>
@@ -543,8 +536,8 @@ int launch_evict(const EvictArgs& a, int num_layers, void* stream)
 {
     const int64_t units = int64_t(num_layers) * a.c.num_requests * a.c.hd;
     // long requests take more threads: the passes over the weights are a chain
-    const int err = a.max_len > 4096 ? run(kvx_select_kernel<1024>, units, 1024, a, stream)
-                                     : run(kvx_select_kernel<256>, units, 256, a, stream);
+    const int err = a.max_len > 4096 ? launch_kernel(kvx_select_kernel<1024>, units, 1024, stream, a)
+                                     : launch_kernel(kvx_select_kernel<256>, units, 256, stream, a);
     if (err) return err;
     MoveArgs m = {};
     m.c = a.c;
@@ -554,8 +547,8 @@ int launch_evict(const EvictArgs& a, int num_layers, void* stream)
     m.lg_lanes = row_lanes(a.c.row_bytes);
     m.lens = a.lens;
     m.max_len = a.max_len;
-    return a.c.row_bytes % 256 ? run(kvx_move_kernel<false>, 2 * units, kWg, m, stream)
-                               : run(kvx_move_kernel<true>, 2 * units, kWg, m, stream);
+    return a.c.row_bytes % 256 ? launch_kernel(kvx_move_kernel<false>, 2 * units, kWg, stream, m)
+                               : launch_kernel(kvx_move_kernel<true>, 2 * units, kWg, stream, m);
 }
 
 int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void* stream)
@@ -571,7 +564,7 @@ int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void*
     m.new_lens = a.new_lens;
     // at least one plane's workgroups, which write new_lens
     const int64_t groups = std::max<int64_t>(1, (2 * int64_t(num_layers) + kHold - 1) / kHold);
-    return run(kvx_commit_kernel, groups * c.num_requests, kWg, m, stream);
+    return launch_kernel(kvx_commit_kernel, groups * c.num_requests, kWg, stream, m);
 }
 
 }  // namespace kvx

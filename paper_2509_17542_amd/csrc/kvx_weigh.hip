@@ -185,10 +185,8 @@ int go_as(const AttendArgs& a, void* stream)
 {
     constexpr int kSlots = kWaves * 32 * kHalves;
     const int tiles = (a.b.max_context + kSlots - 1) / kSlots;
-    kvx_weigh_kernel<kBf16, kCodes, DP, kGeneral, kHalves>
-        <<<dim3(uint32_t(tiles) * a.c.hd * a.c.num_requests), dim3(64 * kWaves), 0,
-           static_cast<hipStream_t>(stream)>>>(a, tiles);
-    return int(hipGetLastError());
+    return launch_kernel(kvx_weigh_kernel<kBf16, kCodes, DP, kGeneral, kHalves>,
+                         int64_t(tiles) * a.c.hd * a.c.num_requests, 64 * kWaves, stream, a, tiles);
 }
 
 template <bool kBf16, int kCodes, int DP>

@@ -55,7 +55,8 @@ __global__ void __launch_bounds__(256) kvx_join_kernel(const AttendArgs a, int l
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int mine = s + k * step + (lane >> lg_lanes);
-                w[k] = mine < n ? __shfl(f, mine & 63) : 0.0f;
+                const float weight = __shfl(f, mine & 63);   // by all lanes: each may hold another's
+                w[k] = mine < n ? weight : 0.0f;
                 x[k] = *reinterpret_cast<const float4*>(from + min(mine, n - 1) * pairs * D);
             }
 #pragma unroll

@@ -101,6 +101,19 @@ def test_head_dims(K, dim, dtype, cache, shape):
     check(p, out, lse)
 
 
+@pytest.mark.parametrize("dim", [16, 64, 80, 128, 256])
+@pytest.mark.parametrize("shape", [dict(new=[1, 2, 1], ctx=[5 * 512 - 3, 700, 29 * 512]),
+                                   dict(new=[1, 1], ctx=[33 * 512 + 7, 41 * 512]),
+                                   dict(new=[37], ctx=[3 * 1024 + 5]),
+                                   dict(new=[9, 20], ctx=[37 * 1024 + 11, 900], tree=3)], ids=str)
+def test_splits(K, dim, shape):
+    """Slots over several workgroups, a number of them that does not divide by the
+    splits a wave joins at once, fewer and more than 32."""
+    p = Problem(dim=dim, heads=1, group=5, seed=dim, **shape)
+    out, lse, _ = run(K, p)
+    check(p, out, lse)
+
+
 @pytest.mark.parametrize("dim", [8, 24, 72, 120, 200, 248])
 def test_head_dims_of_8(K, dim):
     p = Problem(dim=dim, dtype="fp16", cache="fp16", new=[1, 19], ctx=[100, 50], seed=dim)

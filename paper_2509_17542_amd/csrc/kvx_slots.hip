@@ -199,6 +199,7 @@ template <int kThreads_>
 __global__ void __launch_bounds__(kThreads_) kvx_select_kernel(const EvictArgs a)
 {
     constexpr int kW = kThreads_ / 64, kBins = 2048, kPer = kBins / kThreads_;
+    constexpr int kEach = 4;                     // slots of a thread at once
     __shared__ uint32_t s_hist[kBins];
     __shared__ uint32_t s_part[2][kW];
     __shared__ uint32_t s_bin, s_left, s_same;
@@ -229,9 +230,16 @@ __global__ void __launch_bounds__(kThreads_) kvx_select_kernel(const EvictArgs a
             for (int b = tid; b < kBins; b += kThreads_) s_hist[b] = 0;
             __syncthreads();
             const int above = step == 0 ? 32 : step == 1 ? 21 : 10;
-            for (int j = lo + tid; j < hi; j += kThreads_) {
-                const uint32_t k = weight_key(w[j]);
-                if (step == 0 || (k >> above) == (key >> above)) atomicAdd(&s_hist[(k >> shift) & mask], 1u);
+            for (int j0 = lo + tid; j0 < hi; j0 += kEach * kThreads_) {
+                float x[kEach];
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) x[e] = w[min(j0 + e * kThreads_, hi - 1)];
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const uint32_t k = weight_key(x[e]);
+                    if (j0 + e * kThreads_ < hi && (step == 0 || (k >> above) == (key >> above)))
+                        atomicAdd(&s_hist[(k >> shift) & mask], 1u);
+                }
             }
             __syncthreads();
             // thread i holds kPer bins from the top down
@@ -267,14 +275,21 @@ __global__ void __launch_bounds__(kThreads_) kvx_select_kernel(const EvictArgs a
     const bool all_ties = same == left;
     uint32_t ties = 0, out = 0;
     int turn = 0;
-    // counts a flag over the workgroup in slot order: how many before this thread, and in all
-    auto count = [&](bool flag, uint32_t& total) {
-        const uint64_t m = __ballot(flag);
+    // Counts flags over the workgroup in slot order, kEach consecutive slots a thread: how many
+    // lie before this thread's, and in all.
+    auto count = [&](const bool (&flag)[kEach], uint32_t& total) {
+        const uint64_t below = (uint64_t(1) << lane) - 1;
+        uint32_t before = 0, all = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const uint64_t m = __ballot(flag[e]);
+            before += uint32_t(__popcll(m & below));
+            all += uint32_t(__popcll(m));
+        }
         uint32_t* const part = s_part[turn];
         turn ^= 1;                               // the other half may still be read
-        if (lane == 0) part[wave] = uint32_t(__popcll(m));
+        if (lane == 0) part[wave] = all;
         __syncthreads();
-        uint32_t before = uint32_t(__popcll(m & ((uint64_t(1) << lane) - 1)));
         total = 0;
 #pragma unroll
         for (int k = 0; k < kW; ++k) {
@@ -283,31 +298,45 @@ __global__ void __launch_bounds__(kThreads_) kvx_select_kernel(const EvictArgs a
         }
         return before;
     };
-    float x = tid < T ? w[tid] : 0.0f;
-    for (int j0 = 0; j0 < T; j0 += kThreads_) {
-        const int j = j0 + tid;
+    constexpr int kRound = kEach * kThreads_;
+    float x[kEach], next[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) x[e] = w[min(kEach * tid + e, T - 1)];
+    for (int j0 = 0; j0 < T; j0 += kRound) {
+        const int j = j0 + kEach * tid;
         // read ahead of this round's writes: w_out may be w, and they lie below
-        const float next = j + kThreads_ < T ? w[j + kThreads_] : 0.0f;
-        const bool cand = j >= lo && j < hi;
-        const uint32_t k = weight_key(x);
-        bool stay = j < T && (!cand || (any && k > key));
-        const bool tie = any && cand && k == key;
-        if (all_ties) {
-            stay |= tie;
-        } else {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) next[e] = w[min(j + kRound + e, T - 1)];
+        bool stay[kEach], tie[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const bool cand = j + e >= lo && j + e < hi;
+            const uint32_t k = weight_key(x[e]);
+            tie[e] = any && cand && k == key;
+            stay[e] = j + e < T && (!cand || (any && k > key) || (all_ties && tie[e]));
+        }
+        if (!all_ties) {
             uint32_t n;
-            const uint32_t rank = count(tie, n) + ties;
-            stay |= tie && rank < left;
+            uint32_t rank = count(tie, n) + ties;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                stay[e] |= tie[e] && rank < left;
+                rank += tie[e];
+            }
             ties += n;
         }
         uint32_t n;
-        const uint32_t at = count(stay, n) + out;
+        uint32_t at = count(stay, n) + out;
         out += n;
-        if (stay) {
-            kept[at] = j;
-            w_out[at] = x;                       // at <= j: read by every thread already
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            if (stay[e]) {
+                kept[at] = j + e;
+                w_out[at] = x[e];                // at <= j + e: read by every thread already
+                ++at;
+            }
+            x[e] = next[e];
         }
-        x = next;
     }
 }
 

@@ -131,8 +131,17 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
 {
     AttendPlan p = {};
     p.rows = int(std::min<int64_t>(int64_t(b.max_tokens) * (q_heads / c.num_kv_heads), INT32_MAX));
-    // 17 to 32 rows of more than 128 elements do not fit the few-rows kernel's registers
-    p.few = p.rows <= (c.head_dim > 128 ? 16 : 32);
+    const bool eight_bit = c.dtype == KVX_FP8_E4M3FN || c.dtype == KVX_FP8_E5M2;
+    const int64_t heads = int64_t(c.num_requests) * c.num_kv_heads;
+    const int64_t pieces = heads * ((b.max_context + 1023) / 1024);
+    // 17 to 32 rows: the few-rows kernel's registers do not hold more than 128 elements; it cuts
+    // the slots finer, which serves small calls (32 query heads on one KV head, one request of 8000
+    // slots: 17 us, 39 with the other kernel; trees of 4..8 nodes over an fp8 cache of 2048..16384
+    // slots: 128, 133), and where a 16-bit cache's slots fill the card in any case the other kernel
+    // reads them faster (the same trees, 64 of them, bf16: 330 us, 362 with this one; at 512 pieces
+    // both take 48).
+    p.few = p.rows <= 16 || (p.rows <= 32 && c.head_dim <= 128 &&
+                             (eight_bit || pieces < 512));
     p.tile_rows = p.few ? (p.rows <= 16 ? 16 : 32) : p.rows <= 64 ? 64 : 128;
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     if (p.few) {
@@ -143,9 +152,14 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
         // sums have to be written and joined); fewer are split, the bounds counting requests
         // shorter than the longest as idle workgroups (trees of 16..64 nodes over 2048..16384
         // slots: 687 us in one split, 403 with 2048 slots, 392 with 1024, 433 with 512).
-        const int64_t groups = int64_t(c.num_requests) * c.num_kv_heads * p.row_tiles;
+        const int64_t groups = heads * p.row_tiles;
         const int64_t want = groups >= 768 ? 1 : (4096 + groups - 1) / groups;
-        p.chunk = std::max(1024, int((b.max_context + want - 1) / want + 63) & ~63);
+        // Few workgroups in all are cut down to 256 slots, until there is one to a CU (a tree over
+        // 6000 slots, 8 KV heads: 24 us, 48 with 1024 slots at least; one head, 120000 slots: 39,
+        // 54); beyond that the join eats what is won (16 trees over 900 slots: 54 us with two to a
+        // CU, 47 with one).
+        const int64_t least = std::min<int64_t>(1024, std::max<int64_t>(256, groups * b.max_context / 256));
+        p.chunk = int((std::max(least, (b.max_context + want - 1) / want) + 63) & ~int64_t(63));
     }
     p.splits = (b.max_context + p.chunk - 1) / p.chunk;
     return p;

@@ -256,7 +256,6 @@ struct ScoreArgs {
     float c2;        // scale log2(e)
     float to_cap;    // scale 2 log2(e) / softcap: tanh by exp2
     float cap2;      // softcap log2(e)
-    bool general;    // capped or biased
 };
 
 // Scores that are more than a product with a positive scale: the others' largest
@@ -270,7 +269,6 @@ __device__ __forceinline__ ScoreArgs score_args(const AttendArgs& a)
 {
     ScoreArgs s;
     s.c2 = a.scale * kLog2e;
-    s.general = a.softcap > 0.0f || a.slopes != nullptr;
     s.to_cap = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e) / a.softcap : 0.0f;
     s.cap2 = a.softcap > 0.0f ? a.softcap * kLog2e : 0.0f;
     return s;

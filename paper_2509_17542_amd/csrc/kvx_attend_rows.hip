@@ -11,7 +11,24 @@
 //   32 (h: which half of the wave);
 //   O^T = V^T P^T: the weights go on as they lie, 8 of a lane's as one operand;
 //   V is laid out in LDS in that order of slots.
-// Workgroups that read the same slots are dealt to one XCD, next to each other.
+// Where a row's group count is a multiple of 8, workgroups that read the same
+// slots are dealt to one XCD.
+//
+// Bound by the matrix instructions and the exponentials between them: 1024
+// matrix cycles of a SIMD for a tile of 64 slots and 128 rows of 128 elements,
+// 210 (plain scores) to 360 (capped, 8-bit codes) vector instructions, and the
+// wait of one for the other.  8 requests of 2048 tokens on 8192 slots run at 775
+// TFLOP/s in fp16 and 817 in bf16 (a library's large product of that type alone:
+// 1342, 1410); three chunks of 1024..2048 tokens with a bias, a window and a
+// prefix, whose edges cost partial tiles, at 0.71 ms, 710 TFLOP/s; 16 trees of
+// 16..64 nodes over an fp8 cache of 2048..16384 slots, capped scores, at 350 us, and
+// 25 for the join.
+//
+// 128 rows share a tile, 64 slots of it; up to 64 rows have half the waves, so that
+// none only stages, and 32 slots, so that twice as many workgroups fit a CU's LDS.
+// A weight goes to 16 bits for the product with V; its rounding is the type's own
+// half unit in the last place, relative, and the sum of weights that divides is
+// kept in fp32.  Sums, references and outputs stay in fp32 until the end.
 #include <hip/hip_runtime.h>
 
 #include "kvx_attend_dev.h"

@@ -92,14 +92,4 @@ __device__ __forceinline__ uint32_t bits16(float x)
         return __builtin_bit_cast(unsigned short, static_cast<_Float16>(x));
 }
 
-// 8-bit code (byte kByte of a dword) -> fp32, exactly, NaN and infinities included
-template <bool kE5, int kByte>
-__device__ __forceinline__ float value8(uint32_t w)
-{
-    if constexpr (kE5)
-        return __builtin_amdgcn_cvt_f32_bf8(int(w), kByte);
-    else
-        return __builtin_amdgcn_cvt_f32_fp8(int(w), kByte);
-}
-
 }  // namespace kvx

@@ -20,12 +20,14 @@
 // wait of one for the other.  8 requests of 2048 tokens on 8192 slots run at 775
 // TFLOP/s in fp16 and 817 in bf16 (a library's large product of that type alone:
 // 1342, 1410); three chunks of 1024..2048 tokens with a bias, a window and a
-// prefix, whose edges cost partial tiles, at 0.71 ms, 710 TFLOP/s; 16 trees of
-// 16..64 nodes over an fp8 cache of 2048..16384 slots, capped scores, at 350 us, and
-// 25 for the join.
+// prefix, whose edges cost partial tiles, in 0.65 to 0.71 ms, 710 to 765 TFLOP/s; 16
+// trees of 16..64 nodes over an fp8 cache of 2048..16384 slots, capped scores, in
+// 320 to 375 us, 25 of them the join.
 //
 // 128 rows share a tile, 64 slots of it; up to 64 rows have half the waves, so that
-// none only stages, and 32 slots, so that twice as many workgroups fit a CU's LDS.
+// none only stages, and 32 slots, so that twice as many workgroups fit a CU's LDS
+// (trees of 9..16 nodes, 36..64 rows, over the same fp8 cache: 165 us, 190 in workgroups of
+// 128; 64 such over a bf16 cache of 512..8192 slots 303, 340).
 // A weight goes to 16 bits for the product with V; its rounding is the type's own
 // half unit in the last place, relative, and the sum of weights that divides is
 // kept in fp32.  Sums, references and outputs stay in fp32 until the end.

@@ -370,8 +370,9 @@ __device__ __forceinline__ void arrived(Held& v)
 // its own.  The next group's rows are read before this one's are written, and
 // the places of the one after that looked up meanwhile.  Rows of whole 256 bytes
 // are read non-temporal (kOnce): a prompt of 16001 slots cut to 2048 in 32 layers
-// takes 127 us so and 148 without (bf16, rows of 256 bytes); an fp8 batch, rows of
-// 128 bytes, 99 and 91.
+// takes 127 us so and 148 without, both with a slower selection (now 117, the move
+// 93 of it, 5.8 TB/s; bf16, rows of 256 bytes); an fp8 batch, rows of 128 bytes, 99
+// and 91 (the move 78, 5.3 TB/s).
 template <bool kOnce>
 __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
 {

@@ -107,6 +107,8 @@ int join_as(const AttendArgs& a, void* stream)
 
 int join(const AttendArgs& a, bool bf, void* stream)
 {
+    // a request of 120000 slots: 102 us in all, 110 with a wave a pair; 64 of 512..8192: 220, 223
+    // with a workgroup a pair
     if (a.splits > 32) return bf ? join_as<true, 4>(a, stream) : join_as<false, 4>(a, stream);
     return bf ? join_as<true, 1>(a, stream) : join_as<false, 1>(a, stream);
 }

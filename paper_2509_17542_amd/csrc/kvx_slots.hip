@@ -60,24 +60,24 @@ __device__ __forceinline__ uint4 narrow(const float (&x)[8])
     return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
-// A workgroup takes kTokens tokens: their turns (cosine and sine of the fp32
-// angles, reduced in fp64 to a fraction of a turn) go to LDS once for all heads,
-// and each token's place in the cache is looked up by one wave.  A power-of-two
-// group of lanes then covers a head, 8 elements (16 bytes) a lane, whose turns
-// stay in registers for all of a token's heads; the element that a turn pairs
-// with lies in the lane (interleaved) or is read again, out of the cache
-// (halves; pairs that do not fill whole lanes element by element).  Bound by memory for
-// prompts and by its chain of lookups for single tokens.
-template <bool kBf16, int kCache, int kPairing, int kTokens>
+// A workgroup takes a token: its turns (cosine and sine of the fp32 angles,
+// reduced in fp64 to a fraction of a turn) go to LDS once for all heads, and its
+// place in the cache is looked up meanwhile.  A power-of-two group of lanes then
+// covers a head, 8 elements (16 bytes) a lane, whose turns stay in registers for
+// all of the token's heads; the element that a turn pairs with lies in the lane
+// (interleaved) or is read again, out of the cache (halves; pairs that do not fill
+// whole lanes element by element).  Bound by memory for prompts and by its chain
+// of lookups for single tokens.  Prompts of 500..3000 tokens, three axes, into an
+// fp8 cache (250 MB) take 53 us, 4.7 TB/s, and into a bf16 one 60; with four tokens
+// a workgroup 59 and 70.
+template <bool kBf16, int kCache, int kPairing>
 __global__ void __launch_bounds__(kWg) kvx_append_kernel(const AppendArgs a)
 {
-    __shared__ float2 s_turn[kTokens][128];
-    __shared__ int64_t s_row[kTokens];
-    const int t0 = int(blockIdx.x) * kTokens, wave = int(threadIdx.x) >> 6;
+    __shared__ float2 s_turn[128];
+    __shared__ int64_t s_row;
+    const int t = int(blockIdx.x), wave = int(threadIdx.x) >> 6;
     const int D = a.c.dim, P = a.pairs, N = a.b.total_tokens;
-    for (int u = threadIdx.x; u < kTokens * P; u += kWg) {
-        const int k = u / P, i = u - k * P, t = t0 + k;
-        if (t >= N) break;
+    for (int i = threadIdx.x; i < P; i += kWg) {
         int axis = 0;
 #pragma unroll
         for (int s = 0; s < 3; ++s) axis += i >= a.sec_end[s];
@@ -85,94 +85,88 @@ __global__ void __launch_bounds__(kWg) kvx_append_kernel(const AppendArgs a)
         const double turns = double(pos * a.inv_freq[i]) * 0.15915494309189533577;
         float sn, cs;
         sincospif(2.0f * static_cast<float>(turns - rint(turns)), &sn, &cs);
-        s_turn[k][i] = make_float2(cs, sn);
+        s_turn[i] = make_float2(cs, sn);
     }
-    for (int k = wave; k < kTokens; k += kWg / 64) {
-        const int t = t0 + k;
+    if (wave == kWg / 64 - 1) {                  // the pairs are the first waves'
         int64_t row = -1;
-        const int r = t < N ? request_at(a.b.starts, a.c.num_requests, t) : -1;
+        const int r = request_at(a.b.starts, a.c.num_requests, t);
         if (r >= 0 && r < a.c.num_requests) {
             const Request rq = request_of(a.c, a.b, r);
             const int j = rq.ctx + (t - rq.first);
             if (t - rq.first < rq.n && j < rq.total) row = slot_row(a.c, r, j);
         }
-        if ((threadIdx.x & 63) == 0) s_row[k] = row;
+        if ((threadIdx.x & 63) == 0) s_row = row;
     }
     __syncthreads();
     const int per = 1 << a.lg_row, lane = int(threadIdx.x) & (per - 1), e0 = lane * 8;
     const int rows = a.q_heads + 2 * a.c.hd;
     const bool in_row = e0 < D;
+    const int64_t row = s_row;
+    // the turns of this lane's elements: x cs + y sn, the sign of sn with it
+    float cs[8], sn[8];
 #pragma unroll
-    for (int k = 0; k < kTokens; ++k) {
-        const int64_t t = t0 + k;
-        if (t >= N) return;
-        const int64_t row = s_row[k];
-        // the turns of this lane's elements: x cs + y sn, the sign of sn with it
-        float cs[8], sn[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int i = e0 + e;
-            cs[e] = 1.0f, sn[e] = 0.0f;
-            if (i < 2 * P) {
-                const bool second = kPairing == kInterleaved ? i & 1 : i >= P;
-                const float2 x = s_turn[k][kPairing == kInterleaved ? i >> 1 : second ? i - P : i];
-                cs[e] = x.x;
-                sn[e] = second ? x.y : -x.y;
-            }
+    for (int e = 0; e < 8; ++e) {
+        const int i = e0 + e;
+        cs[e] = 1.0f, sn[e] = 0.0f;
+        if (i < 2 * P) {
+            const bool second = kPairing == kInterleaved ? i & 1 : i >= P;
+            const float2 x = s_turn[kPairing == kInterleaved ? i >> 1 : second ? i - P : i];
+            cs[e] = x.x;
+            sn[e] = second ? x.y : -x.y;
         }
-        const bool turned = e0 < 2 * P;          // and so in the row
-        const int other = kPairing == kHalves && turned ? (e0 >= P ? e0 - P : e0 + P) : e0;
-        for (int h = int(threadIdx.x) >> a.lg_row; h < rows; h += kWg >> a.lg_row) {
-            const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.c.hd;
-            const uint16_t* const src = is_q ? a.q + t * a.q_stride + int64_t(h) * D
-                                      : is_v ? a.v + t * a.v_stride + int64_t(h - a.q_heads - a.c.hd) * D
-                                             : a.k + t * a.k_stride + int64_t(h - a.q_heads) * D;
-            // lanes past the row's end hold zeros: the row's maximum takes all of its group
-            float x[8] = {};
-            if (in_row) widen<kBf16>(*reinterpret_cast<const uint4*>(src + e0), x);
-            if (!is_v && turned) {
-                float y[8];
-                if constexpr (kPairing == kInterleaved) {
+    }
+    const bool turned = e0 < 2 * P;              // and so in the row
+    const int other = kPairing == kHalves && turned ? (e0 >= P ? e0 - P : e0 + P) : e0;
+    for (int h = int(threadIdx.x) >> a.lg_row; h < rows; h += kWg >> a.lg_row) {
+        const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.c.hd;
+        const uint16_t* const src = is_q ? a.q + t * a.q_stride + int64_t(h) * D
+                                  : is_v ? a.v + t * a.v_stride + int64_t(h - a.q_heads - a.c.hd) * D
+                                         : a.k + t * a.k_stride + int64_t(h - a.q_heads) * D;
+        // lanes past the row's end hold zeros: the row's maximum takes all of its group
+        float x[8] = {};
+        if (in_row) widen<kBf16>(*reinterpret_cast<const uint4*>(src + e0), x);
+        if (!is_v && turned) {
+            float y[8];
+            if constexpr (kPairing == kInterleaved) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
-                } else if constexpr (kPairing == kHalves) {
-                    widen<kBf16>(*reinterpret_cast<const uint4*>(src + other), y);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int i = e0 + e;
-                        y[e] = i < 2 * P ? value16<kBf16>(src[i >= P ? i - P : i + P]) : 0.0f;
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e0 + e < 2 * P) x[e] = x[e] * cs[e] + y[e] * sn[e];
-            }
-            if (is_q) {
-                // q_out may be q: the head's lanes, all of one wave, have read it
-                __builtin_amdgcn_wave_barrier();
-                if (in_row)
-                    *reinterpret_cast<uint4*>(a.q_out + t * a.q_out_stride + int64_t(h) * D + e0) = narrow<kBf16>(x);
-                continue;
-            }
-            const int kv = is_v ? 1 : 0, head = h - a.q_heads - (is_v ? a.c.hd : 0);
-            char* const dst = a.c.base + kv * a.c.plane_bytes + (row + head) * a.c.row_bytes;
-            if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
-                if (row >= 0 && in_row) *reinterpret_cast<uint4*>(dst + e0 * 2) = narrow<kCache == KVX_BF16>(x);
+                for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+            } else if constexpr (kPairing == kHalves) {
+                widen<kBf16>(*reinterpret_cast<const uint4*>(src + other), y);
             } else {
-                constexpr bool kE5 = kCache == KVX_FP8_E5M2;
-                float m = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) m = fmaxf(m, __builtin_fabsf(x[e]));  // a NaN takes no part
-                m = lanes_max(m, a.lg_row);
-                const float s = m / (kE5 ? 57344.0f : 448.0f);
-                uint32_t w[2] = {0, 0};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e >> 2] |= code8<kE5>(x[e], s) << (8 * (e & 3));
-                if (row >= 0 && in_row) {
-                    *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[0], w[1]);
-                    if (lane == 0) a.c.scales[kv * a.c.plane_scales + row + head] = s;
+                for (int e = 0; e < 8; ++e) {
+                    const int i = e0 + e;
+                    y[e] = i < 2 * P ? value16<kBf16>(src[i >= P ? i - P : i + P]) : 0.0f;
                 }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e0 + e < 2 * P) x[e] = x[e] * cs[e] + y[e] * sn[e];
+        }
+        if (is_q) {
+            // q_out may be q: the head's lanes, all of one wave, have read it
+            __builtin_amdgcn_wave_barrier();
+            if (in_row)
+                *reinterpret_cast<uint4*>(a.q_out + t * a.q_out_stride + int64_t(h) * D + e0) = narrow<kBf16>(x);
+            continue;
+        }
+        const int kv = is_v ? 1 : 0, head = h - a.q_heads - (is_v ? a.c.hd : 0);
+        char* const dst = a.c.base + kv * a.c.plane_bytes + (row + head) * a.c.row_bytes;
+        if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
+            if (row >= 0 && in_row) *reinterpret_cast<uint4*>(dst + e0 * 2) = narrow<kCache == KVX_BF16>(x);
+        } else {
+            constexpr bool kE5 = kCache == KVX_FP8_E5M2;
+            float m = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, __builtin_fabsf(x[e]));  // a NaN takes no part
+            m = lanes_max(m, a.lg_row);
+            const float s = m / (kE5 ? 57344.0f : 448.0f);
+            uint32_t w[2] = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e >> 2] |= code8<kE5>(x[e], s) << (8 * (e & 3));
+            if (row >= 0 && in_row) {
+                *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[0], w[1]);
+                if (lane == 0) a.c.scales[kv * a.c.plane_scales + row + head] = s;
             }
         }
     }
@@ -521,10 +515,7 @@ __global__ void __launch_bounds__(kWg) kvx_commit_kernel(const MoveArgs a)
 template <bool kBf16, int kCache, int kPairing>
 int append_by(const AppendArgs& a, void* stream)
 {
-    // four tokens share a workgroup's start where there are workgroups enough for the card
-    const int64_t n = a.b.total_tokens;
-    return n >= 2048 ? launch_kernel(kvx_append_kernel<kBf16, kCache, kPairing, 4>, (n + 3) / 4, kWg, stream, a)
-                     : launch_kernel(kvx_append_kernel<kBf16, kCache, kPairing, 1>, n, kWg, stream, a);
+    return launch_kernel(kvx_append_kernel<kBf16, kCache, kPairing>, a.b.total_tokens, kWg, stream, a);
 }
 
 template <bool kBf16, int kCache>
@@ -565,7 +556,9 @@ int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream)
 int launch_evict(const EvictArgs& a, int num_layers, void* stream)
 {
     const int64_t units = int64_t(num_layers) * a.c.num_requests * a.c.hd;
-    // long requests take more threads: the passes over the weights are a chain
+    // long requests take more threads, the passes over the weights being a chain (16001 slots, 32
+    // layers: 119 us, 143 with 256 threads); short ones do not fill them (1100..1160 slots, 24
+    // requests in 4 layers: 90 us, 107 with 1024 threads)
     const int err = a.max_len > 4096 ? launch_kernel(kvx_select_kernel<1024>, units, 1024, stream, a)
                                      : launch_kernel(kvx_select_kernel<256>, units, 256, stream, a);
     if (err) return err;

@@ -114,6 +114,23 @@ def test_splits(K, dim, shape):
     check(p, out, lse)
 
 
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3fn")])
+def test_many_requests_of_few_rows(K, dtype, cache):
+    """512 pairs of a request and a KV head, at most 20 rows each, many far fewer."""
+    p = Problem(dim=64, heads=8, group=4, dtype=dtype, cache=cache, tree=2,
+                new=[1 + r % 5 if r % 7 else 0 for r in range(64)], ctx=[(37 * r) % 211 for r in range(64)], seed=5)
+    out, lse, _ = run(K, p)
+    check(p, out, lse)
+
+
+@pytest.mark.parametrize("ctx", [[219], [257], [700], [1500], [6001, 5]])
+def test_short_calls_of_many_rows(K, ctx):
+    """Few workgroups in all: slots cut finer than elsewhere, short requests idle."""
+    p = Problem(dim=128, heads=1, group=4, dtype="fp16", cache="fp16", tree=4, new=[37, 12][:len(ctx)], ctx=ctx, seed=6)
+    out, lse, _ = run(K, p)
+    check(p, out, lse)
+
+
 @pytest.mark.parametrize("dim", [8, 24, 72, 120, 200, 248])
 def test_head_dims_of_8(K, dim):
     p = Problem(dim=dim, dtype="fp16", cache="fp16", new=[1, 19], ctx=[100, 50], seed=dim)

@@ -131,9 +131,10 @@ kvx_status kvx_append(const kvx_cache *cache, const kvx_batch *batch, const kvx_
  *   lse:       device fp32 [N][q_heads] or NULL: log of the sum of exp(x).
  *   workspace: device, >= kvx_attend_workspace bytes, 16-byte aligned; NULL if
  *              that is 0.  Its contents need not be kept between calls.
- * A token that sees no slot gives zeros and an lse of -infinity.  What lies in
- * slots that a token does not see (infinities and NaN too) has no part in its
- * result.  Scores, softmax statistics and sums are fp32; weights are rounded to
+ * A token that sees no slot, or whose scores are all -infinity, gives zeros and an
+ * lse of -infinity; a NaN among its scores (from q or from a key that it sees)
+ * gives NaN in both.  What lies in slots that a token does not see (infinities and
+ * NaN too) has no part in its result.  Scores, softmax statistics and sums are fp32; weights are rounded to
  * 16 bits for the product with V, the output once to dtype.  A 16-bit cache must have the type of q
  * (KVX_EUNSUPPORTED otherwise); q_heads is a multiple of Hd with at most 1024
  * query heads per KV head. */
@@ -148,7 +149,8 @@ kvx_status kvx_attend_workspace(const kvx_cache *cache, const kvx_batch *batch, 
 /* The attention weight of the cache's slots: for KV head g and slot j of
  * request r, the sum over the batch's tokens and the query heads of g of
  * exp(x - lse), with x and visibility as in kvx_attend and lse what that call
- * gave (a token with lse -infinity weighs nothing).
+ * gave (a token with lse -infinity weighs nothing, one with lse NaN makes the sums
+ * of the slots that it sees NaN).
  *   weights: device fp32 [num_requests][Hd][w_stride], w_stride >= max_context:
  *            slots j < C_r have the sum added, the new tokens' slots are set to
  *            it, others are not touched. */

@@ -293,6 +293,13 @@ __device__ __forceinline__ float general_score(const ScoreArgs& s, float dot, fl
 // bits down to 2^-20 of the row's largest.  The shift cancels in the quotient.
 template <bool kBf16>
 constexpr float kShift = kBf16 ? 0.0f : 6.0f;
+// What stands for the reference of a sum of weights l: -inf where l is 0 (nothing
+// seen) and NaN where l is NaN, since m, a maximum, passes NaN by.  The sums of
+// waves and of splits are joined by it.
+__device__ __forceinline__ float reference_of(float m, float l)
+{
+    return l == 0.0f ? -INFINITY : l != l ? l : m;
+}
 // A row's reference m is moved only when a score passes it by more than this:
 // weights stay below 2^(kSlack + kShift), far inside both types.
 constexpr float kSlack = 8.0f;

@@ -449,6 +449,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
     for (int rt = 0; rt < RT; ++rt) {
         l[rt] += __shfl_xor(l[rt], 16);
         l[rt] += __shfl_xor(l[rt], 32);
+        m[rt] = reference_of(m[rt], l[rt]);
         if (g == 0) {
             s_ml[wave][rt * 16 + n16][0] = m[rt];
             s_ml[wave][rt * 16 + n16][1] = l[rt];
@@ -504,7 +505,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
             out[0] = make_float4(x[0], x[1], x[2], x[3]);
             out[1] = make_float4(x[4], x[5], x[6], x[7]);
             if (d == 0) {
-                part_ml[2 * at] = top;
+                part_ml[2 * at] = reference_of(top, total);
                 part_ml[2 * at + 1] = total;
             }
         } else {

@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     if (a.splits > 1) {
         const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
         if (half == 0) {
-            a.part_ml[2 * (split * pairs + at)] = l == 0.0f ? -INFINITY : m;
+            a.part_ml[2 * (split * pairs + at)] = reference_of(m, l);
             a.part_ml[2 * (split * pairs + at) + 1] = l;
         }
         if (l == 0.0f) return;

@@ -304,4 +304,34 @@ __device__ __forceinline__ float reference_of(float m, float l)
 // weights stay below 2^(kSlack + kShift), far inside both types.
 constexpr float kSlack = 8.0f;
 
+// fp16 weights over 8-bit codes.  What is rounded is a weight times its slot's
+// scale, and scales may lie any number of powers of two apart.  Each row takes
+// these products 2^lift times as large, so that the largest of them so far lies
+// between 2^kLiftTop and 2^kLiftMost: those down to 2^-25 of it keep their 11 bits.
+// lift falls when a product would pass 2^kLiftMost; when the reference m rises by
+// d, lift rises by d as well and the sums of V stay as they are, so that what the
+// new reference has made small does not keep the others down.  Only slots that the
+// row sees count.  The weights themselves are formed 2^kLiftShift times smaller
+// there: no product with a finite scale overflows.
+constexpr float kLiftTop = 11.0f, kLiftMost = 15.0f, kLiftMax = 126.0f, kLiftShift = 16.0f;
+
+// the lift of a row whose largest product, not yet lifted, is `most`
+__device__ __forceinline__ float lift_of(float lift, float most)
+{
+    return most > 0.0f ? fminf(lift, kLiftTop - __builtin_amdgcn_logf(most)) : lift;
+}
+
+// what brings a row's sums of V back
+__device__ __forceinline__ float unlifted(float lift, float more = 0.0f)
+{
+    return __builtin_amdgcn_exp2f(fminf(kLiftShift - lift + more, 127.0f));
+}
+
+// |x| where it is finite, else 0
+__device__ __forceinline__ float finite_size(float x)
+{
+    const float a = __builtin_fabsf(x);
+    return a < INFINITY ? a : 0.0f;
+}
+
 }  // namespace kvx

@@ -20,8 +20,9 @@
 // A plain stream of 256-byte pieces at 2 KB strides reads 6.4 TB/s, so what is left
 // is the chunks' ends: places looked up before the first row, sums written after
 // the last, and idle chunks of requests shorter than the longest.
-// A weight goes to 16 bits for the product with V, half a unit in the last place
-// of its own; the sum of weights that divides is kept in fp32, as all sums are.
+// A weight (8-bit codes: times its slot's scale) goes to 16 bits for the product with
+// V, half a unit in the last place of its own; the sum of weights that divides is kept
+// in fp32, as all sums are.
 #include <hip/hip_runtime.h>
 
 #include "kvx_attend_dev.h"
@@ -99,7 +100,8 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
     using T = Tile<kCodes, DP>;
     constexpr int DT = T::DT, kRows = 16 * RT;
     constexpr bool k8 = kCodes != kCodes16;
-    constexpr bool kRef = k8 && !kBf16;             // fp16 weights take V's scale relative to one
+    constexpr bool kLift = k8 && !kBf16;
+    constexpr float kUp = kLift ? kShift<kBf16> - kLiftShift : kShift<kBf16>;
     constexpr int kKeyBytes = kMaxChunk * (k8 ? 20 : 12);
     constexpr int kSlabBytes = 2 * kRows * DP * 4;
     __shared__ __attribute__((aligned(16))) char smem[kKeyBytes > kSlabBytes ? kKeyBytes : kSlabBytes];
@@ -172,11 +174,12 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
     }
     const ScoreArgs sc = score_args(a);
     f32x4 o[RT][DT];
-    float m[RT], l[RT], ref = 0.0f;
+    float m[RT], l[RT], lift[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         m[rt] = -INFINITY;
         l[rt] = 0.0f;
+        lift[rt] = kLiftMax;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[rt][t] = f32x4{0, 0, 0, 0};
     }
@@ -280,21 +283,6 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
                     vs[s][i] = s_vs[at + 16 * s + 4 * g + i];
                 }
         }
-        float fresh_ref = 0.0f;
-        if constexpr (kRef) {
-            // the scales' largest, as a power of two that is not below it
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float y = __builtin_fabsf(vs[s][i]);
-                    fresh_ref = fmaxf(fresh_ref, y < INFINITY ? y : 0.0f);
-                }
-            fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 16));
-            fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 32));
-            const uint32_t e = (__float_as_uint(fresh_ref) + 0x7FFFFFu) & 0x7F800000u;
-            fresh_ref = __uint_as_float(min(max(e, 0x00800000u), 0x7E800000u));
-        }
         put_k(x);
         load_k(next, x);               // the next turn's keys take their place
         f32x4 s[RT][2];
@@ -346,20 +334,22 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, y[e][i]);
-            const bool grow = kRef && fresh_ref > ref;
-            if (__any(top > m[rt] + kSlack) || grow) {
+            if (__any(top > m[rt] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float to = fmaxf(m[rt], top);
                 float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - to);
                 l[rt] *= alpha;
+                if constexpr (kLift) {
+                    const float up = to == -INFINITY ? lift[rt] : fminf(lift[rt] + (to - m[rt]), kLiftMax);
+                    if (to != -INFINITY) alpha = __builtin_amdgcn_exp2f((m[rt] - to) + (up - lift[rt]));
+                    lift[rt] = up;
+                }
                 m[rt] = to;
-                if (grow) alpha *= ref / fresh_ref;
 #pragma unroll
                 for (int t = 0; t < DT; ++t) o[rt][t] *= alpha;
             }
-            const float base = (m[rt] == -INFINITY ? 0.0f : m[rt]) - kShift<kBf16>;
-            const float per_ref = kRef ? 1.0f / fmaxf(ref, fresh_ref) : 1.0f;
+            const float base = (m[rt] == -INFINITY ? 0.0f : m[rt]) - kUp;
             float p[2][4];
 #pragma unroll
             for (int e = 0; e < 2; ++e)
@@ -367,8 +357,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
                 for (int i = 0; i < 4; ++i) {
                     p[e][i] = __builtin_amdgcn_exp2f(y[e][i] - base);
                     l[rt] += p[e][i];
-                    if constexpr (kRef) p[e][i] *= vs[e][i] * per_ref;
-                    else if constexpr (k8) p[e][i] *= vs[e][i];
+                    if constexpr (k8) p[e][i] *= vs[e][i];
                 }
             if (k8 && !whole) {
                 // a scale of a slot that is not seen may be anything
@@ -378,10 +367,29 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
                     for (int i = 0; i < 4; ++i)
                         if (!(mine >> (16 * e + i) & 1u)) p[e][i] = 0.0f;
             }
+            if constexpr (kLift) {
+                float most = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) most = fmaxf(most, finite_size(p[e][i]));
+                if (__any(most * __builtin_amdgcn_exp2f(lift[rt]) > 32768.0f)) {   // 2^kLiftMost
+                    most = fmaxf(most, __shfl_xor(most, 16));
+                    most = fmaxf(most, __shfl_xor(most, 32));
+                    const float to = lift_of(lift[rt], most), by = __builtin_amdgcn_exp2f(to - lift[rt]);
+                    lift[rt] = to;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) o[rt][t] *= by;
+                }
+                const float by = __builtin_amdgcn_exp2f(lift[rt]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[e][i] *= by;
+            }
             pf[rt] = u32x4{pack2<kBf16>(p[0][0], p[0][1]), pack2<kBf16>(p[0][2], p[0][3]),
                            pack2<kBf16>(p[1][0], p[1][1]), pack2<kBf16>(p[1][2], p[1][3])};
         }
-        if constexpr (kRef) ref = fmaxf(ref, fresh_ref);
         if (!whole) {
             drop_v(x, valid);
             uint32_t found = 0;
@@ -449,6 +457,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
     for (int rt = 0; rt < RT; ++rt) {
         l[rt] += __shfl_xor(l[rt], 16);
         l[rt] += __shfl_xor(l[rt], 32);
+        if constexpr (kLift) l[rt] *= 65536.0f;          // 2^kLiftShift
         m[rt] = reference_of(m[rt], l[rt]);
         if (g == 0) {
             s_ml[wave][rt * 16 + n16][0] = m[rt];
@@ -463,8 +472,9 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_ml[w][rt * 16 + n16][0]);
-        scale[rt] = m[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[rt] - top);
-        if constexpr (kRef) scale[rt] *= ref;
+        scale[rt] = m[rt] == -INFINITY ? 0.0f
+                    : kLift            ? unlifted(lift[rt], m[rt] - top)
+                                       : __builtin_amdgcn_exp2f(m[rt] - top);
     }
 #pragma unroll
     for (int half = 0; half < 2; ++half) {

@@ -28,9 +28,9 @@
 // none only stages, and 32 slots, so that twice as many workgroups fit a CU's LDS
 // (trees of 9..16 nodes, 36..64 rows, over the same fp8 cache: 165 us, 190 in workgroups of
 // 128; 64 such over a bf16 cache of 512..8192 slots 303, 340).
-// A weight goes to 16 bits for the product with V; its rounding is the type's own
-// half unit in the last place, relative, and the sum of weights that divides is
-// kept in fp32.  Sums, references and outputs stay in fp32 until the end.
+// A weight (8-bit codes: times its slot's scale) goes to 16 bits for the product with
+// V; its rounding is the type's own half unit in the last place, relative, and the sum
+// of weights that divides is kept in fp32.  Sums, references and outputs stay in fp32 until the end.
 #include <hip/hip_runtime.h>
 
 #include "kvx_attend_dev.h"
@@ -65,7 +65,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     using S = Shape<kCodes, DP, NW>;
     constexpr int KT = S::KT, kWg = S::kWg, ST = KT / 32, DTB = DP / 32;
     constexpr bool k8 = kCodes != kCodes16;
-    constexpr bool kRef = k8 && !kBf16;
+    constexpr bool kLift = k8 && !kBf16;
+    constexpr float kUp = kLift ? kShift<kBf16> - kLiftShift : kShift<kBf16>;
     constexpr uint64_t kAll = KT == 64 ? ~uint64_t(0) : (uint64_t(1) << (KT & 63)) - 1;
     __shared__ __attribute__((aligned(16))) char s_k[2][KT * S::kKRow];
     __shared__ __attribute__((aligned(16))) char s_v[2][DP * S::kVRow];
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     for (int t = 0; t < DTB; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
-    float m = -INFINITY, l = 0.0f, ref = 0.0f;
+    float m = -INFINITY, l = 0.0f, lift = kLiftMax;
 
     const char* const kb = a.c.base;
     const char* const vb = a.c.base + a.c.plane_bytes;
@@ -302,8 +303,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 s[e] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(kl + e * 32 * S::kKRow + c * 32), q[c], s[e]);
         // Scores relative to the row's reference so far; element i of s[e] is slot
         // 32 e + 8 (i / 4) + 4 half + i % 4.
-        float base = (m == -INFINITY ? 0.0f : m) - kShift<kBf16>;
-        float fresh_ref = 0.0f;
+        float base = (m == -INFINITY ? 0.0f : m) - kUp;
         float by = scale2;                       // what the products are still to be multiplied by
         if constexpr (k8) {
             by = 1.0f;
@@ -317,14 +317,6 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     for (int i = 0; i < 4; ++i)
                         s[e][4 * b + i] = kScores != kPlain ? s[e][4 * b + i] * ks[i]
                                                           : __builtin_fmaf(s[e][4 * b + i], ks[i], -base);
-                    if constexpr (kRef) {
-                        const f32x4 vs = *reinterpret_cast<const f32x4*>(s_vs + ring * KT + at);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float y = __builtin_fabsf(vs[i]);
-                            fresh_ref = fmaxf(fresh_ref, y < INFINITY ? y : 0.0f);
-                        }
-                    }
                 }
         }
         if constexpr (kScores != kPlain) {
@@ -393,20 +385,18 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         for (int e = 0; e < ST; ++e)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[e][i]);
-        if constexpr (kRef) {
-            fresh_ref = fmaxf(fresh_ref, __shfl_xor(fresh_ref, 32));
-            const uint32_t e = (__float_as_uint(fresh_ref) + 0x7FFFFFu) & 0x7F800000u;
-            fresh_ref = __uint_as_float(min(max(e, 0x00800000u), 0x7E800000u));
-        }
-        const bool grow = kRef && fresh_ref > ref;
-        if (__any(top > (m == -INFINITY ? -INFINITY : kSlack + kShift<kBf16>)) || grow) {
+        if (__any(top > (m == -INFINITY ? -INFINITY : kSlack + kUp))) {
             top = fmaxf(top, __shfl_xor(top, 32));
             const float to = fmaxf(m, top + base);
             float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-            const float by2 = base - ((to == -INFINITY ? 0.0f : to) - kShift<kBf16>);
+            const float by2 = base - ((to == -INFINITY ? 0.0f : to) - kUp);
             l *= alpha;
+            if constexpr (kLift) {
+                const float up = to == -INFINITY ? lift : fminf(lift + (to - m), kLiftMax);
+                if (to != -INFINITY) alpha = __builtin_amdgcn_exp2f((m - to) + (up - lift));
+                lift = up;
+            }
             m = to;
-            if (grow) alpha *= ref / fresh_ref;
 #pragma unroll
             for (int t2 = 0; t2 < DTB; ++t2) o[t2] *= alpha;
 #pragma unroll
@@ -414,29 +404,60 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[e][i] += by2;
         }
-        if constexpr (kRef) ref = fmaxf(ref, fresh_ref);
-        const float per_ref = kRef ? 1.0f / ref : 1.0f;
+        // weights, times their slots' scales
+        auto weights = [&](int e, int b, float (&p)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(s[e][4 * b + i]);
+                l += p[i];
+            }
+            if constexpr (k8) {
+                const f32x4 vs = *reinterpret_cast<const f32x4*>(s_vs + ring * KT + 32 * e + 8 * b + 4 * half);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] *= vs[i];
+                if (!whole) {
+                    // a scale of a slot that is not seen may be anything
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(mine >> (32 * e + 8 * b + i) & 1)) p[i] = 0.0f;
+                }
+            }
+        };
+        float by_lift = 1.0f;
+        if constexpr (kLift) {
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < ST; ++e)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    float p[4];
+                    weights(e, b, p);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        s[e][4 * b + i] = p[i];
+                        most = fmaxf(most, finite_size(p[i]));
+                    }
+                }
+            if (__any(most * __builtin_amdgcn_exp2f(lift) > 32768.0f)) {   // 2^kLiftMost
+                const float to_lift = lift_of(lift, fmaxf(most, __shfl_xor(most, 32)));
+                const float by_o = __builtin_amdgcn_exp2f(to_lift - lift);
+                lift = to_lift;
+#pragma unroll
+                for (int t2 = 0; t2 < DTB; ++t2) o[t2] *= by_o;
+            }
+            by_lift = __builtin_amdgcn_exp2f(lift);
+        }
         u32x4 pf[ST][2];
 #pragma unroll
         for (int e = 0; e < ST; ++e)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 float p[4];
+                if constexpr (kLift) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(s[e][4 * b + i]);
-                    l += p[i];
-                }
-                if constexpr (k8) {
-                    const f32x4 vs = *reinterpret_cast<const f32x4*>(s_vs + ring * KT + 32 * e + 8 * b + 4 * half);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[i] *= kRef ? vs[i] * per_ref : vs[i];
-                    if (!whole) {
-                        // a scale of a slot that is not seen may be anything
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (!(mine >> (32 * e + 8 * b + i) & 1)) p[i] = 0.0f;
-                    }
+                    for (int i = 0; i < 4; ++i) p[i] = s[e][4 * b + i] * by_lift;
+                } else {
+                    weights(e, b, p);
                 }
                 pf[e][b >> 1][2 * (b & 1)] = pack2<kBf16>(p[0], p[1]);
                 pf[e][b >> 1][2 * (b & 1) + 1] = pack2<kBf16>(p[2], p[3]);
@@ -520,6 +541,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     }
 
     l += __shfl_xor(l, 32);
+    if constexpr (kLift) l *= 65536.0f;              // 2^kLiftShift
+    const float back = kLift ? unlifted(lift) : 1.0f;
     if (!live) return;
     const int64_t at = token * a.q_heads + head;
     if (a.splits > 1) {
@@ -537,11 +560,11 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 const int d = 32 * t + 8 * b + 4 * half;
                 f32x4 x;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = kRef ? o[t][4 * b + i] * ref : o[t][4 * b + i];
+                for (int i = 0; i < 4; ++i) x[i] = kLift ? o[t][4 * b + i] * back : o[t][4 * b + i];
                 if (d < D) *reinterpret_cast<f32x4*>(out + d) = x;
             }
     } else {
-        const float inv = l == 0.0f ? 0.0f : (kRef ? ref : 1.0f) / l;
+        const float inv = l == 0.0f ? 0.0f : back / l;
         uint16_t* const out = a.out + token * a.out_stride + int64_t(head) * D;
 #pragma unroll
         for (int t = 0; t < DTB; ++t)

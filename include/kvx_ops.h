@@ -133,7 +133,10 @@ kvx_status kvx_append(const kvx_cache *cache, const kvx_batch *batch, const kvx_
  *              that is 0.  Its contents need not be kept between calls.
  * A token that sees no slot, or whose scores are all -infinity, gives zeros and an
  * lse of -infinity; a NaN among its scores (from q or from a key that it sees)
- * gives NaN in both.  What lies in slots that a token does not see (infinities and
+ * gives NaN in both.  An infinite value in a slot that it sees makes that element of
+ * the result infinite however small the slot's weight is, opposite infinities or a
+ * NaN make it NaN (a score of -infinity leaves open whether its slot's values
+ * count).  What lies in slots that a token does not see (infinities and
  * NaN too) has no part in its result.  Scores, softmax statistics and sums are fp32; weights are rounded to
  * 16 bits for the product with V, the output once to dtype.  A 16-bit cache must have the type of q
  * (KVX_EUNSUPPORTED otherwise); q_heads is a multiple of Hd with at most 1024

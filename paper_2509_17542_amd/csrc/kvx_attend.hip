@@ -44,9 +44,10 @@ __global__ void __launch_bounds__(256) kvx_join_kernel(const AttendArgs a, int l
     float acc[4] = {}, total = 0.0f;
     for (int s0 = begin; s0 < end; s0 += 64) {
         const float2 v = s0 + lane < end ? ml[(s0 + lane) * pairs + at] : make_float2(-INFINITY, 0.0f);
-        const float f = v.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(v.x - top);
-        total += f == 0.0f ? 0.0f : v.y * f;
-        const uint64_t some = __ballot(f != 0.0f);
+        // a split that saw nothing left no sum: -1
+        const float f = v.x == -INFINITY ? -1.0f : __builtin_amdgcn_exp2f(v.x - top);
+        total += f < 0.0f ? 0.0f : v.y * f;
+        const uint64_t some = __ballot(!(f < 0.0f));
         const int n = some ? 64 - __builtin_clzll(some) : 0;
         const float* const from = a.part_o + (int64_t(s0) * pairs + at) * D + (d < D ? d : 0);
         for (int s = 0; s < n; s += 4 * step) {
@@ -56,13 +57,14 @@ __global__ void __launch_bounds__(256) kvx_join_kernel(const AttendArgs a, int l
             for (int k = 0; k < 4; ++k) {
                 const int mine = s + k * step + (lane >> lg_lanes);
                 const float weight = __shfl(f, mine & 63);   // by all lanes: each may hold another's
-                w[k] = mine < n ? weight : 0.0f;
+                w[k] = mine < n ? weight : -1.0f;
                 x[k] = *reinterpret_cast<const float4*>(from + min(mine, n - 1) * pairs * D);
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (w[k] != 0.0f)       // a split that saw nothing left no sum
-                    acc[0] += x[k].x * w[k], acc[1] += x[k].y * w[k], acc[2] += x[k].z * w[k], acc[3] += x[k].w * w[k];
+                if (!(w[k] < 0.0f))
+                    acc[0] += weighted(x[k].x, w[k]), acc[1] += weighted(x[k].y, w[k]),
+                        acc[2] += weighted(x[k].z, w[k]), acc[3] += weighted(x[k].w, w[k]);
             }
         }
     }

@@ -96,10 +96,11 @@ __device__ __forceinline__ uint32_t pair16(uint32_t key0, uint32_t key1)
 // ---- non-finite values ---------------------------------------------------------
 //
 // A weight of 0 does not hide an infinity from a matrix product (0 x inf is
-// NaN).  Where a tile is not seen whole by every row, the product takes its
-// finite values only; if there were others, a second walk over such tiles, after
-// the first, finds by three products of ones with the rows' visibility which
-// sums have +inf, -inf or NaN among their terms.
+// NaN), whether the slot is not seen or its weight came to 0.  Where a tile is not
+// seen whole by every row, the product takes its finite values only.  If there were
+// others, or a sum of a tile seen whole is not finite, a second walk finds by three
+// products of ones with the rows' visibility which sums have +inf, -inf or NaN
+// among their terms, and these become that.
 
 template <bool kBf16>
 constexpr uint32_t kOne = kBf16 ? 0x3F80u : 0x3C00u;
@@ -145,11 +146,55 @@ __device__ __forceinline__ u32x4 classify8(u32x4 v, int kind)
                  classify2<kBf16>(v.z, kind), classify2<kBf16>(v.w, kind)};
 }
 
-// a sum `o` that the product of kind `kind` says had such values among its terms
-__device__ __forceinline__ float with_special(float o, float count, int kind)
+// an 8-bit slot's scale as its codes that are not finite take it, and all of its
+// codes where it is not finite itself: 1, -1, 0, +-inf or NaN
+__device__ __forceinline__ float scale_kind(float s)
 {
-    return count > 0.0f ? o + (kind == 1 ? INFINITY : kind == 2 ? -INFINITY : NAN) : o;
+    return s == 0.0f || !(__builtin_fabsf(s) < INFINITY) ? s : __builtin_copysignf(1.0f, s);
 }
+
+// a pair times a factor each
+template <bool kBf16>
+__device__ __forceinline__ uint32_t times2(uint32_t w, float lo, float hi)
+{
+    return bits16<kBf16>(value16<kBf16>(w & 0xFFFFu) * lo) | bits16<kBf16>(value16<kBf16>(w >> 16) * hi) << 16;
+}
+
+// a sum by its weight in a join; one that is not finite stays so where the weight came to 0
+__device__ __forceinline__ float weighted(float x, float w)
+{
+    return w != 0.0f ? x * w : __builtin_fabsf(x) < INFINITY ? 0.0f : x;
+}
+
+// whether one of kT vectors of kN sums is not finite (four chains, not one)
+template <int kN, int kT>
+__device__ __forceinline__ bool any_endless(const float __attribute__((ext_vector_type(kN))) (&o)[kT])
+{
+    float zero[4] = {};
+#pragma unroll
+    for (int t = 0; t < kT; ++t)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) zero[i & 3] = __builtin_fmaf(o[t][i], 0.0f, zero[i & 3]);
+    const float sum = (zero[0] + zero[1]) + (zero[2] + zero[3]);
+    return sum != sum;
+}
+
+// Which of a lane's kN sums have such values among their terms, a bit a sum and kind.
+template <int kN>
+struct Had {
+    uint64_t bits[3][(kN + 63) / 64] = {};
+    __device__ __forceinline__ void add(int at, float count, int kind)
+    {
+        bits[kind - 1][kN <= 64 ? 0 : at >> 6] |= uint64_t(count > 0.0f) << (at & 63);
+    }
+    // what sum `at` is, which the products say is `o`
+    __device__ __forceinline__ float of(int at, float o) const
+    {
+        const int w = kN <= 64 ? 0 : at >> 6, s = at & 63;
+        const bool up = bits[0][w] >> s & 1, down = bits[1][w] >> s & 1, none = bits[2][w] >> s & 1;
+        return none || (up && down) ? NAN : up ? INFINITY : down ? -INFINITY : o;
+    }
+};
 
 // ---- visibility ------------------------------------------------------------------
 

@@ -420,36 +420,66 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
             turn(v, v + kWaves * kTile < v1 ? v + kWaves * kTile : v, x);
         }
     }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) special |= __any(live[rt] && any_endless<4, DT>(o[rt])) != 0;
     if (__builtin_expect(special, 0)) {
-        // the tiles that not every row sees whole again: which sums had infinities or NaN
+        // the tiles again, an element of V's rows at a time: which sums had infinities or NaN
+        // (the lane's number hidden from the compiler, and what follows from it formed anew: values
+        // kept for this path cost the first walk registers)
+        int hidden = lane;
+        __asm__ volatile("" : "+v"(hidden));
+        const int n16 = hidden & 15, g = hidden >> 4;
+        Had<4 * DT> had[RT];
+#pragma unroll 1
         for (v = v0 + wave * kTile; v < v1; v += kWaves * kTile) {
             const uint32_t valid = valid_of(v);
-            if (is_whole(v, valid)) continue;
-            T x;
-            load_v(v, x);
-            drop_v(x, valid);
+#pragma unroll 1
+            for (int t = 0; t < DT; ++t) {
+                const int byte = (n16 * DT + t) * T::kEl, at = byte < a.c.row_bytes ? byte : 0;
+                u32x4 f = {0, 0, 0, 0};
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const uint32_t mine = seen_by(rt, v, valid);
-                u32x4 seen;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t two = mine >> (16 * (w >> 1) + 2 * (w & 1)) & 3u;
-                    seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
+                for (int j = 0; j < 8; ++j) {
+                    const int slot = 16 * (j >> 2) + 4 * g + (j & 3);
+                    const char* const from = vb + s_off[v - v0 + slot] + at;
+                    uint32_t x;
+                    if constexpr (k8)
+                        x = times2<kBf16>(widen2<kBf16, kCodes, false>(*reinterpret_cast<const uint8_t*>(from)),
+                                          scale_kind(s_vs[v - v0 + slot]), 0.0f) & 0xFFFFu;
+                    else
+                        x = *reinterpret_cast<const uint16_t*>(from);
+                    f[j >> 1] |= (valid >> slot & 1u ? x : 0u) << (16 * (j & 1));
                 }
+                uint32_t some = 0;
 #pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    const u32x4 f = v_operand(x, t);
+                for (int p = 0; p < 4; ++p) some |= nonfinite<kBf16, kCodes16>(f[p]);
+                if (!__any(some != 0)) continue;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const int row = rt * 16 + n16, i = int(fast_div(uint32_t(row < rows ? row : 0), a.div_group));
+                    const int pos = a.b.positions ? a.b.positions[rq.first + i] : rq.ctx + i;
+                    const uint32_t mine =
+                        row < rows ? uint32_t(seen_of(a, rq, r, i, pos, rg.slot(v), valid)) >> (4 * g) : 0u;
+                    u32x4 seen;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t two = mine >> (16 * (w >> 1) + 2 * (w & 1)) & 3u;
+                        seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
+                    }
 #pragma unroll
                     for (int kind = 1; kind <= 3; ++kind) {
                         const f32x4 count = mfma16<kBf16>(classify8<kBf16>(f, kind), seen, f32x4{0, 0, 0, 0});
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[rt][t][i] = with_special(o[rt][t][i], count[i], kind);
+                        for (int i = 0; i < 4; ++i) had[rt].add(4 * t + i, count[i], kind);
                     }
-                    __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
                 }
             }
         }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rt][t][i] = had[rt].of(4 * t + i, o[rt][t][i]);
     }
 
     // the waves' sums, joined through LDS two at a time
@@ -476,6 +506,16 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
                     : kLift            ? unlifted(lift[rt], m[rt] - top)
                                        : __builtin_amdgcn_exp2f(m[rt] - top);
     }
+    if (__builtin_expect(special, 0)) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rt][t][i] = weighted(o[rt][t][i], scale[rt]);
+            scale[rt] = 1.0f;
+        }
+    }
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         if ((wave >> 1) == half) {
@@ -486,7 +526,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
 #pragma unroll
                     for (int t = 0; t < DT; ++t) {
                         float* const at = slab + (rt * 16 + n16) * DP + (4 * g + i) * DT + t;
-                        const float x = scale[rt] == 0.0f ? 0.0f : o[rt][t][i] * scale[rt];
+                        const float x = o[rt][t][i] * scale[rt];
                         *at = half == 0 ? x : *at + x;
                     }
         }

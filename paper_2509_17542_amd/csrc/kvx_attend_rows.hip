@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     __shared__ __attribute__((aligned(16))) float s_ks[k8 ? 2 * kWg : 1];
     __shared__ __attribute__((aligned(16))) float s_vs[k8 ? 2 * kWg : 1];
     __shared__ uint64_t s_valid[S::kRing];
-    __shared__ int s_special;
+    __shared__ int s_special, s_some[2][NW];
 
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         return w;
     };
     // kind 0: K, and V with its values that are not finite as 0 where not every row sees the
-    // tile whole; 1 to 3: ones where V is +inf, -inf, NaN
+    // tile whole; 1 to 3: ones where V (8-bit: a code times its slot's scale) is +inf, -inf, NaN
     auto store = [&](int t, uint64_t valid, int kind) {
         char* const ks = s_k[t & 1];
         char* const vs = s_v[t & 1];
@@ -273,8 +273,15 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 if (found && kind == 0) s_special = 1;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    *reinterpret_cast<u32x4*>(out + e * S::kVRow) =
-                        kind == 0 && !found ? column(x, e) : classify8<kBf16>(column(x, e), kind);
+                    u32x4 w = column(x, e);
+                    if (k8 && kind != 0) {
+                        const float* const at = s_vs + (t & (S::kRing - 1)) * KT + first;
+#pragma unroll
+                        for (int p = 0; p < 4; ++p)
+                            w[p] = times2<kBf16>(w[p], scale_kind(at[2 * (p & 1) + 8 * (p >> 1)]),
+                                                 scale_kind(at[2 * (p & 1) + 8 * (p >> 1) + 1]));
+                    }
+                    *reinterpret_cast<u32x4*>(out + e * S::kVRow) = kind == 0 && !found ? w : classify8<kBf16>(w, kind);
                     __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
                 }
             }
@@ -495,18 +502,43 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             if (busy) use(t, valid);
             valid = next_valid;
         }
+        if (live && any_endless<16, DTB>(o)) s_special = 1;
         __syncthreads();
         if (__builtin_expect(s_special, 0)) {
-            // the tiles that not every row sees whole again: which sums had infinities or NaN
+            // the tiles again: which sums had infinities or NaN
+            Had<16 * DTB> had;
             for (int t = 0; t < tiles; ++t) {
                 if (t % S::kBatch == 0) {
                     __syncthreads();
                     look_up(t / S::kBatch);
                     note_places(t / S::kBatch);
+                    note_scales(t / S::kBatch);
                     __syncthreads();
                 }
                 valid = valid_of(t);
-                if (whole_tile(t, valid)) continue;
+                places(t);
+                load();
+                bool some = false;
+#pragma unroll
+                for (int i = 0; i < S::kVPer; ++i) {
+                    const int kg = min((tid + i * kWg) / (DP / 4), KT / 8 - 1), first = (kg >> 1) * 16 + (kg & 1) * 4;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int slot = first + (e & 3) + (e >> 2) * 8;
+                        if (!(valid >> slot & 1)) continue;
+                        some |= nonfinite<kBf16, kCodes>(vr[i][e].x) != 0;
+                        if constexpr (!k8) some |= nonfinite<kBf16, kCodes>(vr[i][e].y) != 0;
+                        if constexpr (k8)
+                            some |= !(__builtin_fabsf(s_vs[(t & (S::kRing - 1)) * KT + slot]) < INFINITY);
+                    }
+                }
+                const bool some_here = __any(some) != 0;
+                if (lane == 0) s_some[t & 1][wave] = some_here;
+                __syncthreads();
+                some = false;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) some |= s_some[t & 1][w] != 0;
+                if (!some) continue;
                 const uint64_t mine = live ? seen_by_me(t, valid) : 0;
                 for (int kind = 1; kind <= 3; ++kind) {
                     places(t);
@@ -531,12 +563,16 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                                                   seen, count);
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[t2][i] = with_special(o[t2][i], count[i], kind);
+                        for (int i = 0; i < 16; ++i) had.add(16 * t2 + i, count[i], kind);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     __syncthreads();
                 }
             }
+#pragma unroll
+            for (int t = 0; t < DTB; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] = had.of(16 * t + i, o[t][i]);
         }
     }
 

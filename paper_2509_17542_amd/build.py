@@ -25,7 +25,8 @@ DEVICE = ["-x", "hip", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-
 SOURCES = [("kvx_kernels.hip", True), ("kvx_plan.cpp", False), ("kvx_pipe.cpp", False),
            ("kvx_pd.cpp", False), ("kvx_ops.cpp", False), ("kvx_slots.hip", True),
            ("kvx_attend.hip", True), ("kvx_attend_few.hip", True),
-           ("kvx_attend_rows.hip", True), ("kvx_weigh.hip", True)]
+           ("kvx_attend_rows_16.hip", True), ("kvx_attend_rows_e4m3.hip", True),
+           ("kvx_attend_rows_e5m2.hip", True), ("kvx_weigh.hip", True)]
 
 
 def build(verbose: bool = False) -> str:

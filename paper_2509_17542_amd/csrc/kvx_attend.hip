@@ -115,6 +115,15 @@ int join(const AttendArgs& a, bool bf, void* stream)
     return bf ? join_as<true, 1>(a, stream) : join_as<false, 1>(a, stream);
 }
 
+int rows(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream)
+{
+    switch (cache_dtype) {
+    case KVX_FP8_E4M3FN: return launch_rows<kCodesE4m3>(a, p, dtype, stream);
+    case KVX_FP8_E5M2: return launch_rows<kCodesE5m2>(a, p, dtype, stream);
+    default: return launch_rows<kCodes16>(a, p, dtype, stream);
+    }
+}
+
 }  // namespace
 
 int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int cache_dtype,
@@ -127,7 +136,7 @@ int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int c
     a.part_ml = static_cast<float*>(workspace);
     a.part_o = a.part_ml + 2 * plan_pairs(a, p);
     const int err = p.few ? launch_few(a, p, dtype, cache_dtype, stream)
-                          : launch_rows(a, p, dtype, cache_dtype, stream);
+                          : rows(a, p, dtype, cache_dtype, stream);
     return err || p.splits == 1 ? err : join(a, bf, stream);
 }
 

@@ -301,21 +301,34 @@ struct ScoreArgs {
     float c2;        // scale log2(e)
     float to_cap;    // scale 2 log2(e) / softcap: tanh by exp2
     float cap2;      // softcap log2(e)
+    float by_cap;    // 1 / softcap
 };
 
-// Scores that are more than a product with a positive scale: the others' largest
-// is found before they are scaled.
-inline bool general_scores(const AttendArgs& a)
+// What scores are beside the product: nothing (and a positive scale); biased, capped
+// or of another scale; those with a cap above kWideCap.
+enum Scores : int { kPlain = 0, kGeneral = 1, kWide = 2 };
+
+// Caps up to here take tanh in the form whose error is absolute, 2^-22 of the cap: in
+// units of the score no more than 1.5e-5, below a weight's own rounding.  Larger
+// ones take another, in kernels of their own: beside it in the same ones it costs the
+// smaller caps registers (weights of a prompt's last 32 tokens 69 us, 62 apart; trees
+// over an fp8 cache 349, 337).
+constexpr float kWideCap = 64.0f;
+
+inline Scores scores_of(const AttendArgs& a)
 {
-    return a.softcap > 0.0f || a.slopes || !(a.scale > 0.0f);
+    return a.softcap > kWideCap ? kWide : a.softcap > 0.0f || a.slopes || !(a.scale > 0.0f) ? kGeneral : kPlain;
 }
 
 __device__ __forceinline__ ScoreArgs score_args(const AttendArgs& a)
 {
+    constexpr float kMost = 3.402823466e38f;
     ScoreArgs s;
     s.c2 = a.scale * kLog2e;
-    s.to_cap = a.softcap > 0.0f ? a.scale * (2.0f * kLog2e) / a.softcap : 0.0f;
+    // finite also for the smallest caps: a score of 0 stays 0
+    s.to_cap = a.softcap > 0.0f ? fmaxf(fminf(a.scale * (2.0f * kLog2e) / a.softcap, kMost), -kMost) : 0.0f;
     s.cap2 = a.softcap > 0.0f ? a.softcap * kLog2e : 0.0f;
+    s.by_cap = a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f;
     return s;
 }
 
@@ -327,10 +340,23 @@ __device__ __forceinline__ float capped(const ScoreArgs& s, float e2y, float mor
                           s.cap2 + more);
 }
 
+// The same from the score x2 for any cap: an error of 2^-20 of the score.  Up to
+// |y| = 1/4 the series of tanh, whose next term is 2^-21 of y there.
+__device__ __forceinline__ float capped_wide(const ScoreArgs& s, float x2, float more)
+{
+    const float y = x2 * (kLn2 * s.by_cap), z = y * y;
+    const float near = x2 * __builtin_fmaf(-z, __builtin_fmaf(-z, __builtin_fmaf(-z, 17.0f / 315.0f, 2.0f / 15.0f),
+                                                              1.0f / 3.0f), 1.0f);
+    return __builtin_fabsf(y) < 0.25f ? near + more : capped(s, x2 * (2.0f * s.by_cap), more);
+}
+
 // The product's x2, capped and biased; slope2 is the head's slope log2(e).
+template <int kScores>
 __device__ __forceinline__ float general_score(const ScoreArgs& s, float dot, float slope2, int distance)
 {
-    const float x = s.cap2 > 0.0f ? capped(s, dot * s.to_cap, 0.0f) : dot * s.c2;
+    const float x = kScores == kWide ? capped_wide(s, dot * s.c2, 0.0f)
+                    : s.cap2 > 0.0f  ? capped(s, dot * s.to_cap, 0.0f)
+                                     : dot * s.c2;
     return x - slope2 * static_cast<float>(distance < 0 ? -distance : distance);
 }
 

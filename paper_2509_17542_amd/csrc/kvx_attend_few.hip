@@ -94,7 +94,7 @@ struct Tile {
 template <int kCodes, int DP, int RT>
 constexpr int kWavesPerSimd = DP >= 256 ? 1 : DP * RT >= 256 || (DP >= 128 && kCodes == kCodes16) ? 2 : 3;
 
-template <bool kBf16, int kCodes, int DP, int RT, bool kGeneral>
+template <bool kBf16, int kCodes, int DP, int RT, int kScores>
 __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_attend_few_kernel(const AttendArgs a)
 {
     using T = Tile<kCodes, DP>;
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             float y[2][4], top = -INFINITY;
-            if constexpr (!kGeneral) {
+            if constexpr (kScores == kPlain) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -318,8 +318,8 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        y[e][i] = general_score(sc, k8 ? s[rt][e][i] * ks[e][i] : s[rt][e][i], slope2[rt],
-                                                qpos[rt] - s_pos[at + 16 * e + 4 * g + i]);
+                        y[e][i] = general_score<kScores>(sc, k8 ? s[rt][e][i] * ks[e][i] : s[rt][e][i], slope2[rt],
+                                                         qpos[rt] - s_pos[at + 16 * e + 4 * g + i]);
             }
             uint32_t mine = ~0u;
             if (!whole) {
@@ -572,18 +572,21 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
     }
 }
 
-template <bool kBf16, int kCodes, int DP, int RT, bool kGeneral>
+template <bool kBf16, int kCodes, int DP, int RT, int kScores>
 int go_as(const AttendArgs& a, void* stream)
 {
-    return launch_kernel(kvx_attend_few_kernel<kBf16, kCodes, DP, RT, kGeneral>,
+    return launch_kernel(kvx_attend_few_kernel<kBf16, kCodes, DP, RT, kScores>,
                          int64_t(a.c.num_requests) * a.splits * a.c.hd, kWg, stream, a);
 }
 
 template <bool kBf16, int kCodes, int DP, int RT>
 int go(const AttendArgs& a, void* stream)
 {
-    return general_scores(a) ? go_as<kBf16, kCodes, DP, RT, true>(a, stream)
-                                        : go_as<kBf16, kCodes, DP, RT, false>(a, stream);
+    switch (scores_of(a)) {
+    case kWide: return go_as<kBf16, kCodes, DP, RT, kWide>(a, stream);
+    case kGeneral: return go_as<kBf16, kCodes, DP, RT, kGeneral>(a, stream);
+    default: return go_as<kBf16, kCodes, DP, RT, kPlain>(a, stream);
+    }
 }
 
 template <bool kBf16, int kCodes>

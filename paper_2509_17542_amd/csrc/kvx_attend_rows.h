@@ -1,5 +1,6 @@
 // Attention of many query rows per KV head (wide trees, chains) over the paged
-// cache.
+// cache; each type of cache is a source of its own (kvx_attend_rows_*.hip), which
+// includes this one.
 //
 // A workgroup takes 32 rows per wave (rows are tokens times the query heads of
 // a KV head, tokens outermost) of one request and KV head, and walks the
@@ -31,6 +32,8 @@
 // A weight (8-bit codes: times its slot's scale) goes to 16 bits for the product with
 // V; its rounding is the type's own half unit in the last place, relative, and the sum
 // of weights that divides is kept in fp32.  Sums, references and outputs stay in fp32 until the end.
+#pragma once
+
 #include <hip/hip_runtime.h>
 
 #include "kvx_attend_dev.h"
@@ -38,9 +41,9 @@
 namespace kvx {
 namespace {
 
-// What scores are beside the product: nothing (and a positive scale), biased (or
-// another scale), capped (and perhaps biased).
-enum Scores : int { kPlain = 0, kBiased = 1, kCapped = 2 };
+// Here scores with a cap (and perhaps a bias) are kept apart from those with a bias
+// alone (or another scale).
+enum RowsScores : int { kBiased = kGeneral, kCappedWide = kWide, kCapped = 3 };
 
 template <int kCodes, int DP, int NW>
 struct Shape {
@@ -121,8 +124,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         }
     }
     const ScoreArgs sc = score_args(a);
-    constexpr bool cap = kScores == kCapped;
-    const float scale2 = cap ? sc.to_cap : sc.c2;
+    const float scale2 = kScores == kCapped ? sc.to_cap : sc.c2;
     f32x16 o[DTB];
 #pragma unroll
     for (int t = 0; t < DTB; ++t)
@@ -330,11 +332,16 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             const int j0 = rg.slot(tile_at(t));
             const bool in_order = !a.b.positions || j0 + KT <= rq.ctx;  // slot j lies at position j
             const bool linear = kScores == kBiased && in_order && __all(qpos - j0 >= KT);
-            if constexpr (cap) {
+            if constexpr (kScores == kCapped) {
 #pragma unroll
                 for (int e = 0; e < ST; ++e)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[e][i] = capped(sc, s[e][i] * by, -base);
+            } else if constexpr (kScores == kCappedWide) {
+#pragma unroll
+                for (int e = 0; e < ST; ++e)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[e][i] = capped_wide(sc, s[e][i] * by, -base);
             } else if (linear) {
                 // all slots before the token: linear in the slot
                 const float first = slope2 * static_cast<float>(j0 + 4 * half - qpos) - base;
@@ -628,9 +635,13 @@ int go_as(const AttendArgs& a, const AttendPlan& p, void* stream)
 template <bool kBf16, int kCodes, int DP, int NW>
 int go(const AttendArgs& a, const AttendPlan& p, void* stream)
 {
-    if (a.softcap > 0.0f) return go_as<kBf16, kCodes, DP, NW, kCapped>(a, p, stream);
-    return general_scores(a) ? go_as<kBf16, kCodes, DP, NW, kBiased>(a, p, stream)
-                             : go_as<kBf16, kCodes, DP, NW, kPlain>(a, p, stream);
+    switch (scores_of(a)) {
+    case kWide: return go_as<kBf16, kCodes, DP, NW, kCappedWide>(a, p, stream);
+    case kGeneral:
+        return a.softcap > 0.0f ? go_as<kBf16, kCodes, DP, NW, kCapped>(a, p, stream)
+                                : go_as<kBf16, kCodes, DP, NW, kBiased>(a, p, stream);
+    default: return go_as<kBf16, kCodes, DP, NW, kPlain>(a, p, stream);
+    }
 }
 
 template <bool kBf16, int kCodes>
@@ -644,14 +655,10 @@ int pick(const AttendArgs& a, const AttendPlan& p, void* stream)
 
 }  // namespace
 
-int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream)
+template <int kCodes>
+int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, void* stream)
 {
-    const bool bf = dtype == KVX_BF16;
-    switch (cache_dtype) {
-    case KVX_FP8_E4M3FN: return bf ? pick<true, kCodesE4m3>(a, p, stream) : pick<false, kCodesE4m3>(a, p, stream);
-    case KVX_FP8_E5M2: return bf ? pick<true, kCodesE5m2>(a, p, stream) : pick<false, kCodesE5m2>(a, p, stream);
-    default: return bf ? pick<true, kCodes16>(a, p, stream) : pick<false, kCodes16>(a, p, stream);
-    }
+    return dtype == KVX_BF16 ? pick<true, kCodes>(a, p, stream) : pick<false, kCodes>(a, p, stream);
 }
 
 }  // namespace kvx

@@ -127,7 +127,8 @@ struct AttendPlan {
 };
 AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
 int launch_few(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream);
-int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream);
+template <int kCodes>
+int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, void* stream);
 
 // Each enqueues its kernels on `stream` and returns a hipError_t value.
 int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream);

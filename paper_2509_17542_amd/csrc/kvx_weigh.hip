@@ -23,19 +23,19 @@ namespace {
 constexpr int kWaves = 4;
 
 // kHalves: 32 slots each; two are held in registers
-template <bool kBf16, int kCodes, int DP, bool kGeneral, int kHalves>
+template <bool kBf16, int kCodes, int DP, int kScores, int kHalves>
 __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : kHalves == 2 ? 3 : 4))
     kvx_weigh_kernel(const AttendArgs a, int tiles)
 {
     constexpr int kKeys = 32 * kHalves, kTiles16 = 2 * kHalves;
-    constexpr bool kHeld = kHalves == 2;
+    constexpr bool kHeld = kHalves == 2, kOther = kScores != kPlain;
     constexpr bool k8 = kCodes != kCodes16;
     constexpr int kEl = k8 ? 1 : 2, NC = DP / 32;
     constexpr int kRow = DP * kEl, kRowPieces = kRow / 16, kLoads = 32 * kRow / 1024;
     __shared__ __attribute__((aligned(16))) char s_k[kWaves][32 * kRow];
     __shared__ int64_t s_off[kWaves][kKeys];
     __shared__ float s_ks[kWaves][kKeys];
-    __shared__ int32_t s_pos[kWaves][kGeneral ? kKeys : 1];
+    __shared__ int32_t s_pos[kWaves][kOther ? kKeys : 1];
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, g = lane >> 4;
     const int D = a.c.dim, G = a.group;
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : kHalves == 2 ? 3
         // a slot that lies in no page reads the plane's first row, and is masked
         s_off[wave][lane] = my_row < 0 ? 0 : (my_row + h) * a.c.row_bytes;
         if constexpr (k8) s_ks[wave][lane] = my_row < 0 ? 0.0f : a.c.scales[my_row + h];
-        if constexpr (kGeneral) s_pos[wave][lane] = place_of(a, rq, j0 + lane);
+        if constexpr (kOther) s_pos[wave][lane] = place_of(a, rq, j0 + lane);
     }
     // a wave's LDS is its own and its accesses stay in order: nothing to wait for
     __builtin_amdgcn_wave_barrier();
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : kHalves == 2 ? 3
         Rows next;
         if (rows > 16) read_rows(row0 + 16 < rows ? row0 + 16 : 0, next);
         const float lse2 = now.lse == -INFINITY ? INFINITY : now.lse * kLog2e;
-        const float slope2 = kGeneral && a.slopes ? a.slopes[now.head] * kLog2e : 0.0f;
+        const float slope2 = kOther && a.slopes ? a.slopes[now.head] * kLog2e : 0.0f;
         uint64_t mine = now.live && now.lse != -INFINITY ? ~uint64_t(0) : 0;
         if (!whole && mine) mine = seen_of(a, rq, r, now.tok, now.qpos, j0, valid);
         mine >>= 4 * g;
@@ -156,9 +156,9 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : kHalves == 2 ? 3
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float x = s[i] * ks[e][i];
-                if constexpr (kGeneral)
-                    x = general_score(sc, k8 ? s[i] * s_ks[wave][16 * e + 4 * g + i] : s[i], slope2,
-                                      now.qpos - s_pos[wave][16 * e + 4 * g + i]);
+                if constexpr (kOther)
+                    x = general_score<kScores>(sc, k8 ? s[i] * s_ks[wave][16 * e + 4 * g + i] : s[i], slope2,
+                                               now.qpos - s_pos[wave][16 * e + 4 * g + i]);
                 const float p = __builtin_amdgcn_exp2f(x - lse2);
                 v[4 * e + i] += all || (mine >> (16 * e + i) & 1) ? p : 0.0f;
             }
@@ -181,22 +181,30 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : kHalves == 2 ? 3
     if (n16 < kWriters && j < rq.total) *out = j < rq.ctx ? old + w : w;
 }
 
-template <bool kBf16, int kCodes, int DP, bool kGeneral, int kHalves>
+template <bool kBf16, int kCodes, int DP, int kScores, int kHalves>
 int go_as(const AttendArgs& a, void* stream)
 {
     constexpr int kSlots = kWaves * 32 * kHalves;
     const int tiles = (a.b.max_context + kSlots - 1) / kSlots;
-    return launch_kernel(kvx_weigh_kernel<kBf16, kCodes, DP, kGeneral, kHalves>,
+    return launch_kernel(kvx_weigh_kernel<kBf16, kCodes, DP, kScores, kHalves>,
                          int64_t(tiles) * a.c.hd * a.c.num_requests, 64 * kWaves, stream, a, tiles);
+}
+
+template <bool kBf16, int kCodes, int DP, int kScores>
+int go_by(const AttendArgs& a, void* stream)
+{
+    const bool held = int64_t(a.b.max_tokens) * a.group > 16;
+    return held ? go_as<kBf16, kCodes, DP, kScores, 2>(a, stream) : go_as<kBf16, kCodes, DP, kScores, 1>(a, stream);
 }
 
 template <bool kBf16, int kCodes, int DP>
 int go(const AttendArgs& a, void* stream)
 {
-    const bool held = int64_t(a.b.max_tokens) * a.group > 16;
-    if (general_scores(a))
-        return held ? go_as<kBf16, kCodes, DP, true, 2>(a, stream) : go_as<kBf16, kCodes, DP, true, 1>(a, stream);
-    return held ? go_as<kBf16, kCodes, DP, false, 2>(a, stream) : go_as<kBf16, kCodes, DP, false, 1>(a, stream);
+    switch (scores_of(a)) {
+    case kWide: return go_by<kBf16, kCodes, DP, kWide>(a, stream);
+    case kGeneral: return go_by<kBf16, kCodes, DP, kGeneral>(a, stream);
+    default: return go_by<kBf16, kCodes, DP, kPlain>(a, stream);
+    }
 }
 
 template <bool kBf16, int kCodes>

@@ -30,7 +30,9 @@
  * caller's, calls only launch kernels on the given hipStream_t (void*, NULL =
  * default stream) and may be recorded into a HIP graph; a kvx_status comes back
  * and kvx_last_error() has its message.  A call with nothing to do returns
- * KVX_OK without inspecting its data pointers.  Results are the same in every
+ * KVX_OK without inspecting its data pointers; one that would need 2^32 threads or
+ * more in a launch (2^24 workgroups of 256) returns KVX_EUNSUPPORTED before the
+ * first.  Results are the same in every
  * run: no sum depends on the order in which workgroups end.
  */
 #ifndef KVX_OPS_H

@@ -97,21 +97,28 @@ int64_t plan_pairs(const AttendArgs& a, const AttendPlan& p)
     return (int64_t(a.b.total_tokens) * a.q_heads * p.splits + 3) & ~int64_t(3);
 }
 
+// waves of a pair: a request of 120000 slots: 102 us in all, 110 with a wave a pair; 64 of
+// 512..8192: 220, 223 with a workgroup a pair
+int join_waves(int splits) { return splits > 32 ? 4 : 1; }
+
+int64_t join_groups(int32_t tokens, int32_t q_heads, int waves)
+{
+    const int64_t pairs = int64_t(tokens) * q_heads;
+    return waves == 4 ? pairs : (pairs + 3) / 4;
+}
+
 template <bool kBf16, int kWaves>
 int join_as(const AttendArgs& a, void* stream)
 {
-    const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
     int lg_lanes = 0;
     while ((4 << lg_lanes) < a.c.dim) ++lg_lanes;
-    return launch_kernel(kvx_join_kernel<kBf16, kWaves>, kWaves == 4 ? pairs : (pairs + 3) / 4, 256, stream, a,
-                         lg_lanes);
+    return launch_kernel(kvx_join_kernel<kBf16, kWaves>, join_groups(a.b.total_tokens, a.q_heads, kWaves), 256, stream,
+                         a, lg_lanes);
 }
 
 int join(const AttendArgs& a, bool bf, void* stream)
 {
-    // a request of 120000 slots: 102 us in all, 110 with a wave a pair; 64 of 512..8192: 220, 223
-    // with a workgroup a pair
-    if (a.splits > 32) return bf ? join_as<true, 4>(a, stream) : join_as<false, 4>(a, stream);
+    if (join_waves(a.splits) == 4) return bf ? join_as<true, 4>(a, stream) : join_as<false, 4>(a, stream);
     return bf ? join_as<true, 1>(a, stream) : join_as<false, 1>(a, stream);
 }
 
@@ -138,6 +145,15 @@ int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int c
     const int err = p.few ? launch_few(a, p, dtype, cache_dtype, stream)
                           : rows(a, p, dtype, cache_dtype, stream);
     return err || p.splits == 1 ? err : join(a, bf, stream);
+}
+
+double attend_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads, const AttendPlan& p)
+{
+    // the rows kernel has a wave to 32 rows
+    const int threads = p.few ? 256 : 2 * p.tile_rows;
+    const double first = double(c.num_requests) * c.num_kv_heads * p.splits * p.row_tiles * threads;
+    return p.splits == 1 ? first
+                         : std::max(first, double(join_groups(b.total_tokens, q_heads, join_waves(p.splits))) * 256);
 }
 
 AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)

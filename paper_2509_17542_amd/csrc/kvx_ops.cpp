@@ -17,9 +17,6 @@ bool is_16bit(int dt) { return dt == KVX_FP16 || dt == KVX_BF16; }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// workgroups of one launch stay below 2^31
-constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
-
 // slots of one request
 constexpr int32_t kMaxSlots = 1 << 30;
 
@@ -143,6 +140,13 @@ kvx_status need_device()
     return KVX_OK;
 }
 
+// threads of a call's largest launch
+kvx_status check_threads(double threads)
+{
+    if (threads >= 0x1p32) return fail(KVX_EUNSUPPORTED, "%.0f threads in a launch: 2^32 or more", threads);
+    return KVX_OK;
+}
+
 #define KVX_TRY(call)                              \
     do {                                           \
         const kvx_status status_ = (call);         \
@@ -227,6 +231,7 @@ extern "C" kvx_status kvx_append(const kvx_cache* c, const kvx_batch* b, const k
     }
     KVX_TRY(check_rows("k", k, k_stride, kv_width));
     KVX_TRY(check_rows("v", v, v_stride, kv_width));
+    KVX_TRY(check_threads(kvx::append_threads(b->total_tokens)));
     KVX_TRY(need_device());
     kvx::AppendArgs a = {};
     a.c = cache_args(*c, layer);
@@ -281,9 +286,7 @@ extern "C" kvx_status kvx_attend(const kvx_cache* c, const kvx_batch* b, const k
         return fail(KVX_EINVAL, "a 16-byte aligned workspace of %llu bytes is needed, %llu are given",
                     (unsigned long long)need, (unsigned long long)(workspace ? workspace_bytes : 0));
     const kvx::AttendPlan plan = kvx::attend_plan(*c, *b, q_heads);
-    if (int64_t(b->total_tokens) * q_heads > kMaxGrid ||
-        double(c->num_requests) * c->num_kv_heads * plan.splits * plan.row_tiles > double(kMaxGrid))
-        return fail(KVX_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
+    KVX_TRY(check_threads(kvx::attend_threads(*c, *b, q_heads, plan)));
     KVX_TRY(need_device());
     kvx::AttendArgs a = attend_args(*c, *b, *s, layer, q_heads);
     a.q = static_cast<const uint16_t*>(q);
@@ -307,8 +310,7 @@ extern "C" kvx_status kvx_weigh(const kvx_cache* c, const kvx_batch* b, const kv
     if (!lse || !weights) return fail(KVX_EINVAL, "NULL lse or weights");
     if (w_stride < b->max_context)
         return fail(KVX_EINVAL, "w_stride %lld below max_context %d", (long long)w_stride, b->max_context);
-    if ((int64_t(b->max_context) + 63) / 64 * c->num_kv_heads * c->num_requests > kMaxGrid)
-        return fail(KVX_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
+    KVX_TRY(check_threads(kvx::weigh_threads(*c, *b, q_heads)));
     KVX_TRY(need_device());
     kvx::AttendArgs a = attend_args(*c, *b, *s, layer, q_heads);
     a.q = static_cast<const uint16_t*>(q);
@@ -339,11 +341,10 @@ extern "C" kvx_status kvx_evict(const kvx_cache* c, int32_t layer0, int32_t num_
     if (!lens || !weights || !weights_out || !kept || !new_lens)
         return fail(KVX_EINVAL, "NULL lens, weights, weights_out, kept or new_lens");
     if (new_lens == lens) return fail(KVX_EINVAL, "new_lens must be another buffer than lens");
-    if (int64_t(2) * num_layers * c->num_requests * c->num_kv_heads > kMaxGrid)
-        return fail(KVX_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
-    KVX_TRY(need_device());
     kvx::EvictArgs a = {};
     a.c = cache_args(*c, layer0);
+    KVX_TRY(check_threads(kvx::evict_threads(a.c, num_layers, max_len)));
+    KVX_TRY(need_device());
     a.lens = lens;
     a.weights = weights;
     a.weights_out = weights_out;
@@ -369,8 +370,8 @@ extern "C" kvx_status kvx_commit(const kvx_cache* c, int32_t layer0, int32_t num
         return fail(KVX_EINVAL, "NULL contexts, accepted, counts or new_lens");
     if (new_lens == contexts) return fail(KVX_EINVAL, "new_lens must be another buffer than contexts");
     if (num_layers > 0) KVX_TRY(check_buffers(*c));
-    if (int64_t(2) * num_layers * c->num_requests * c->num_kv_heads > kMaxGrid)
-        return fail(KVX_EUNSUPPORTED, "more than 2^31 - 1 workgroups");
+    const kvx::CacheArgs args = cache_args(*c, layer0);
+    KVX_TRY(check_threads(kvx::commit_threads(args, num_layers)));
     KVX_TRY(need_device());
     kvx::CommitArgs a = {};
     a.contexts = contexts;
@@ -378,5 +379,5 @@ extern "C" kvx_status kvx_commit(const kvx_cache* c, int32_t layer0, int32_t num
     a.counts = counts;
     a.new_lens = new_lens;
     a.a_stride = a_stride;
-    return launched(kvx::launch_commit(cache_args(*c, layer0), a, num_layers, stream));
+    return launched(kvx::launch_commit(args, a, num_layers, stream));
 }

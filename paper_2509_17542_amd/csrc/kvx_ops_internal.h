@@ -130,6 +130,14 @@ int launch_few(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dt
 template <int kCodes>
 int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, void* stream);
 
+// The threads of a call's largest launch, workgroups times their size: HIP takes
+// fewer than 2^32.
+double append_threads(int32_t tokens);
+double evict_threads(const CacheArgs& c, int num_layers, int max_len);
+double commit_threads(const CacheArgs& c, int num_layers);
+double attend_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads, const AttendPlan& p);
+double weigh_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
+
 // Each enqueues its kernels on `stream` and returns a hipError_t value.
 int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream);
 int launch_evict(const EvictArgs& a, int num_layers, void* stream);

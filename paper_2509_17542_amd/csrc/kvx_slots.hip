@@ -545,7 +545,27 @@ int row_lanes(int64_t bytes)
     return lg;
 }
 
+// long requests take more threads, the passes over the weights being a chain (16001 slots, 32
+// layers: 119 us, 143 with 256 threads); short ones do not fill them (1100..1160 slots, 24
+// requests in 4 layers: 90 us, 107 with 1024 threads)
+int select_threads(int max_len) { return max_len > 4096 ? 1024 : kWg; }
+
+// workgroups of a commit: at least one plane's, which write new_lens
+int64_t commit_groups(const CacheArgs& c, int num_layers)
+{
+    return std::max<int64_t>(1, (2 * int64_t(num_layers) + kHold - 1) / kHold) * c.num_requests;
+}
+
 }  // namespace
+
+double append_threads(int32_t tokens) { return double(tokens) * kWg; }
+
+double evict_threads(const CacheArgs& c, int num_layers, int max_len)
+{
+    return double(num_layers) * c.num_requests * c.hd * std::max(select_threads(max_len), 2 * kWg);
+}
+
+double commit_threads(const CacheArgs& c, int num_layers) { return double(commit_groups(c, num_layers)) * kWg; }
 
 int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream)
 {
@@ -556,11 +576,8 @@ int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream)
 int launch_evict(const EvictArgs& a, int num_layers, void* stream)
 {
     const int64_t units = int64_t(num_layers) * a.c.num_requests * a.c.hd;
-    // long requests take more threads, the passes over the weights being a chain (16001 slots, 32
-    // layers: 119 us, 143 with 256 threads); short ones do not fill them (1100..1160 slots, 24
-    // requests in 4 layers: 90 us, 107 with 1024 threads)
-    const int err = a.max_len > 4096 ? launch_kernel(kvx_select_kernel<1024>, units, 1024, stream, a)
-                                     : launch_kernel(kvx_select_kernel<256>, units, 256, stream, a);
+    const int err = select_threads(a.max_len) == 1024 ? launch_kernel(kvx_select_kernel<1024>, units, 1024, stream, a)
+                                                      : launch_kernel(kvx_select_kernel<kWg>, units, kWg, stream, a);
     if (err) return err;
     MoveArgs m = {};
     m.c = a.c;
@@ -585,9 +602,7 @@ int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void*
     m.contexts = a.contexts;
     m.counts = a.counts;
     m.new_lens = a.new_lens;
-    // at least one plane's workgroups, which write new_lens
-    const int64_t groups = std::max<int64_t>(1, (2 * int64_t(num_layers) + kHold - 1) / kHold);
-    return launch_kernel(kvx_commit_kernel, groups * c.num_requests, kWg, stream, m);
+    return launch_kernel(kvx_commit_kernel, commit_groups(c, num_layers), kWg, stream, m);
 }
 
 }  // namespace kvx

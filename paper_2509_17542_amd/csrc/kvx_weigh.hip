@@ -181,11 +181,15 @@ __global__ void __launch_bounds__(64 * kWaves, (DP >= 256 ? 2 : kHalves == 2 ? 3
     if (n16 < kWriters && j < rq.total) *out = j < rq.ctx ? old + w : w;
 }
 
+// more than 16 query rows: 64 slots a wave, else 32
+int halves_of(int32_t max_tokens, int32_t group) { return int64_t(max_tokens) * group > 16 ? 2 : 1; }
+
+int tiles_of(int32_t max_context, int halves) { return (max_context + kWaves * 32 * halves - 1) / (kWaves * 32 * halves); }
+
 template <bool kBf16, int kCodes, int DP, int kScores, int kHalves>
 int go_as(const AttendArgs& a, void* stream)
 {
-    constexpr int kSlots = kWaves * 32 * kHalves;
-    const int tiles = (a.b.max_context + kSlots - 1) / kSlots;
+    const int tiles = tiles_of(a.b.max_context, kHalves);
     return launch_kernel(kvx_weigh_kernel<kBf16, kCodes, DP, kScores, kHalves>,
                          int64_t(tiles) * a.c.hd * a.c.num_requests, 64 * kWaves, stream, a, tiles);
 }
@@ -193,8 +197,8 @@ int go_as(const AttendArgs& a, void* stream)
 template <bool kBf16, int kCodes, int DP, int kScores>
 int go_by(const AttendArgs& a, void* stream)
 {
-    const bool held = int64_t(a.b.max_tokens) * a.group > 16;
-    return held ? go_as<kBf16, kCodes, DP, kScores, 2>(a, stream) : go_as<kBf16, kCodes, DP, kScores, 1>(a, stream);
+    return halves_of(a.b.max_tokens, a.group) == 2 ? go_as<kBf16, kCodes, DP, kScores, 2>(a, stream)
+                                                   : go_as<kBf16, kCodes, DP, kScores, 1>(a, stream);
 }
 
 template <bool kBf16, int kCodes, int DP>
@@ -215,6 +219,12 @@ int pick(const AttendArgs& a, void* stream)
 }
 
 }  // namespace
+
+double weigh_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
+{
+    const int tiles = tiles_of(b.max_context, halves_of(b.max_tokens, q_heads / c.num_kv_heads));
+    return double(tiles) * c.num_kv_heads * c.num_requests * (64 * kWaves);
+}
 
 int launch_weigh(const AttendArgs& a, int dtype, int cache_dtype, void* stream)
 {

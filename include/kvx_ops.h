@@ -138,11 +138,12 @@ kvx_status kvx_append(const kvx_cache *cache, const kvx_batch *batch, const kvx_
  * gives NaN in both.  An infinite value in a slot that it sees makes that element of
  * the result infinite however small the slot's weight is, opposite infinities or a
  * NaN make it NaN (a score of -infinity leaves open whether its slot's values
- * count).  What lies in slots that a token does not see (infinities and
- * NaN too) has no part in its result.  Scores, softmax statistics and sums are fp32; weights are rounded to
- * 16 bits for the product with V, the output once to dtype.  A 16-bit cache must have the type of q
- * (KVX_EUNSUPPORTED otherwise); q_heads is a multiple of Hd with at most 1024
- * query heads per KV head. */
+ * count).  What lies in slots that a token does not see (infinities and NaN too) has
+ * no part in its result.  Scores, softmax statistics and sums are fp32.  For the
+ * product with V weights are rounded to 16 bits, with max_tokens * q_heads / Hd <= 16
+ * to twice as many; the output is rounded once to dtype.  A 16-bit cache must have
+ * the type of q (KVX_EUNSUPPORTED otherwise); q_heads is a multiple of Hd with at
+ * most 1024 query heads per KV head. */
 kvx_status kvx_attend(const kvx_cache *cache, const kvx_batch *batch, const kvx_scores *scores,
                       int32_t layer, int32_t dtype, int32_t q_heads, const void *q,
                       int64_t q_stride, void *out, int64_t out_stride, float *lse,

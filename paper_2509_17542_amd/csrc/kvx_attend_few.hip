@@ -20,9 +20,13 @@
 // A plain stream of 256-byte pieces at 2 KB strides reads 6.4 TB/s, so what is left
 // is the chunks' ends: places looked up before the first row, sums written after
 // the last, and idle chunks of requests shorter than the longest.
-// A weight (8-bit codes: times its slot's scale) goes to 16 bits for the product with
-// V, half a unit in the last place of its own; the sum of weights that divides is kept
-// in fp32, as all sums are.
+// For the product with V a weight (8-bit codes: times its slot's scale) is taken as two
+// 16-bit terms, itself rounded and what that left: the reads hide the second product
+// (the calls above: 218.5 us with it and without; over an fp8 cache 154, 153; 256
+// elements 326, 323).  With 17 to 32 rows it is one term, half a unit in the last
+// place of its own, as in the many-rows kernel, which some of those calls take (trees of
+// 8 nodes over an fp8 cache: 217 us with two, 209).  The sum of weights that divides
+// is kept in fp32, as all sums are.
 #include <hip/hip_runtime.h>
 
 #include "kvx_attend_dev.h"
@@ -100,6 +104,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
     using T = Tile<kCodes, DP>;
     constexpr int DT = T::DT, kRows = 16 * RT;
     constexpr bool k8 = kCodes != kCodes16;
+    constexpr bool kTwoTerms = RT == 1;
     constexpr bool kLift = k8 && !kBf16;
     constexpr float kUp = kLift ? kShift<kBf16> - kLiftShift : kShift<kBf16>;
     constexpr int kKeyBytes = kMaxChunk * (k8 ? 20 : 12);
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
                 for (int rt = 0; rt < RT; ++rt) s[rt][e] = mfma16<kBf16>(f, q[rt][c], s[rt][e]);
             }
         }
-        u32x4 pf[RT];
+        u32x4 pf[RT], rest[kTwoTerms ? RT : 1];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             float y[2][4], top = -INFINITY;
@@ -389,6 +394,11 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
             }
             pf[rt] = u32x4{pack2<kBf16>(p[0][0], p[0][1]), pack2<kBf16>(p[0][2], p[0][3]),
                            pack2<kBf16>(p[1][0], p[1][1]), pack2<kBf16>(p[1][2], p[1][3])};
+            if constexpr (kTwoTerms)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    rest[rt][w] = pack2<kBf16>(p[w >> 1][2 * (w & 1)] - value16<kBf16>(pf[rt][w] & 0xFFFFu),
+                                               p[w >> 1][2 * (w & 1) + 1] - value16<kBf16>(pf[rt][w] >> 16));
         }
         if (!whole) {
             drop_v(x, valid);
@@ -407,7 +417,10 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
         for (int t = 0; t < DT; ++t) {
             const u32x4 f = v_operand(x, t);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma16<kBf16>(f, pf[rt], o[rt][t]);
+            for (int rt = 0; rt < RT; ++rt) {
+                o[rt][t] = mfma16<kBf16>(f, pf[rt], o[rt][t]);
+                if constexpr (kTwoTerms) o[rt][t] = mfma16<kBf16>(f, rest[rt], o[rt][t]);
+            }
         }
     };
 

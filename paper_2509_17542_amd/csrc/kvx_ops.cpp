@@ -370,14 +370,15 @@ extern "C" kvx_status kvx_commit(const kvx_cache* c, int32_t layer0, int32_t num
         return fail(KVX_EINVAL, "NULL contexts, accepted, counts or new_lens");
     if (new_lens == contexts) return fail(KVX_EINVAL, "new_lens must be another buffer than contexts");
     if (num_layers > 0) KVX_TRY(check_buffers(*c));
-    const kvx::CacheArgs args = cache_args(*c, layer0);
-    KVX_TRY(check_threads(kvx::commit_threads(args, num_layers)));
-    KVX_TRY(need_device());
     kvx::CommitArgs a = {};
+    a.c = cache_args(*c, layer0);
+    KVX_TRY(check_threads(kvx::commit_threads(a.c, num_layers)));
+    KVX_TRY(need_device());
     a.contexts = contexts;
     a.accepted = accepted;
     a.counts = counts;
     a.new_lens = new_lens;
     a.a_stride = a_stride;
-    return launched(kvx::launch_commit(args, a, num_layers, stream));
+    a.num_layers = num_layers;
+    return launched(kvx::launch_commit(a, stream));
 }

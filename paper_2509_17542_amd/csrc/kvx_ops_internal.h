@@ -1,5 +1,6 @@
 // Internal declarations shared by the host side of the decode operators
-// (kvx_ops.cpp) and their kernels (kvx_slots.hip, kvx_attend.hip).
+// (kvx_ops.cpp) and their kernels: kvx_slots.hip (append, evict, commit),
+// kvx_attend.hip with kvx_attend_few.hip and kvx_attend_rows*, kvx_weigh.hip.
 #pragma once
 
 #include <cstdint>
@@ -68,30 +69,31 @@ struct EvictArgs {
     int32_t max_len, budget, sink, recent;
 };
 
-struct CommitArgs {
-    const int32_t* contexts;
-    const int32_t* accepted;
-    const int32_t* counts;
-    int32_t* new_lens;
-    int32_t a_stride;
+// What an eviction moves: in every plane and head, row i of request r takes row
+// kept[i], for `budget` rows where lens[r] is above that, else none.
+struct MoveArgs {
+    CacheArgs c;
+    const int32_t* kept;         // [layer][request][head][budget], ascending
+    const int32_t* lens;
+    int32_t budget;
+    int32_t max_len;
+    int32_t lg_lanes;            // log2 of the lanes that a head's row takes
     int32_t pad;
 };
 
-// Rows that move up inside their request: row first + i takes row first +
-// index[i], index ascending.
-struct MoveArgs {
+// In every plane, row contexts[r] + i of request r takes row contexts[r] +
+// accepted[i], all heads, for a path of counts[r] entries or fewer, whose end goes
+// to new_lens[r].
+struct CommitArgs {
     CacheArgs c;
-    const int32_t* index;        // evict: [layer][request][head][stride]; commit: [request][stride]
-    int32_t stride;
-    int32_t num_layers;
-    int32_t max_len;
-    int32_t lg_lanes;            // log2 of the lanes that a row takes
-    // evict: `stride` rows of request r where lens[r] is above that, else none; commit: a path of
-    // counts[r] entries or fewer, from slot contexts[r] on, whose end goes to new_lens[r]
-    const int32_t* lens;
     const int32_t* contexts;
+    const int32_t* accepted;     // [request][a_stride], ascending
     const int32_t* counts;
     int32_t* new_lens;
+    int32_t a_stride;
+    int32_t num_layers;
+    int32_t lg_lanes;            // log2 of the lanes that all heads' rows take
+    int32_t pad;
 };
 
 struct AttendArgs {
@@ -141,7 +143,7 @@ double weigh_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
 // Each enqueues its kernels on `stream` and returns a hipError_t value.
 int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream);
 int launch_evict(const EvictArgs& a, int num_layers, void* stream);
-int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void* stream);
+int launch_commit(const CommitArgs& a, void* stream);
 int launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype,
                   void* workspace, void* stream);
 int launch_weigh(const AttendArgs& a, int dtype, int cache_dtype, void* stream);

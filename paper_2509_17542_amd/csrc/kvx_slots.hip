@@ -1,6 +1,7 @@
 // gfx950 kernels that write and move rows of the paged cache: kvx_append (the
-// new tokens' rows, with rotary positions), kvx_evict (selection by weight) and
-// the move of rows up their request, shared by kvx_evict and kvx_commit.
+// new tokens' rows, with rotary positions), kvx_evict (selection by weight, then
+// the move of what stays, a head's rows at a time) and kvx_commit (the move of a
+// path's rows, all heads at a time).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -379,9 +380,9 @@ __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
     u /= R;
     const int kv = u & 1, layer = u >> 1;
     const int T = min(min(max(a.lens[r], 0), a.max_len), a.c.row_slots);
-    const int rows = T > a.stride ? a.stride : 0;
+    const int rows = T > a.budget ? a.budget : 0;
     if (rows == 0) return;
-    const int32_t* const index = a.index + ((int64_t(layer) * R + r) * H + h) * a.stride;
+    const int32_t* const index = a.kept + ((int64_t(layer) * R + r) * H + h) * a.budget;
     const int64_t plane = int64_t(2) * layer + kv;
     char* const base = a.c.base + plane * a.c.plane_bytes;
     float* const scales = a.c.scales ? a.c.scales + plane * a.c.plane_scales : nullptr;
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
 
 // Commit: one workgroup per request and kHold planes; rows of all heads lie side
 // by side, and a lane holds one piece of a row in every plane.
-__global__ void __launch_bounds__(kWg) kvx_commit_kernel(const MoveArgs a)
+__global__ void __launch_bounds__(kWg) kvx_commit_kernel(const CommitArgs a)
 {
     __shared__ int64_t s_src[kWg], s_dst[kWg];
     const int tid = int(threadIdx.x), lane = tid & 63, R = a.c.num_requests;
@@ -452,8 +453,8 @@ __global__ void __launch_bounds__(kWg) kvx_commit_kernel(const MoveArgs a)
     const int planes = min(kHold, 2 * a.num_layers - plane0);
     // the path's length: entries ascend strictly and their slots lie in the row
     const int first = max(a.contexts[r], 0);
-    const int32_t* const index = a.index + int64_t(r) * a.stride;
-    const int most = min(a.counts[r], a.stride);
+    const int32_t* const index = a.accepted + int64_t(r) * a.a_stride;
+    const int most = min(a.counts[r], a.a_stride);
     int rows = 0;
     while (rows < most) {
         const int i = rows + lane;
@@ -581,9 +582,8 @@ int launch_evict(const EvictArgs& a, int num_layers, void* stream)
     if (err) return err;
     MoveArgs m = {};
     m.c = a.c;
-    m.index = a.kept;
-    m.stride = a.budget;
-    m.num_layers = num_layers;
+    m.kept = a.kept;
+    m.budget = a.budget;
     m.lg_lanes = row_lanes(a.c.row_bytes);
     m.lens = a.lens;
     m.max_len = a.max_len;
@@ -591,18 +591,11 @@ int launch_evict(const EvictArgs& a, int num_layers, void* stream)
                                : launch_kernel(kvx_move_kernel<true>, 2 * units, kWg, stream, m);
 }
 
-int launch_commit(const CacheArgs& c, const CommitArgs& a, int num_layers, void* stream)
+int launch_commit(const CommitArgs& given, void* stream)
 {
-    MoveArgs m = {};
-    m.c = c;
-    m.index = a.accepted;
-    m.stride = a.a_stride;
-    m.num_layers = num_layers;
-    m.lg_lanes = row_lanes(int64_t(c.hd) * c.row_bytes);
-    m.contexts = a.contexts;
-    m.counts = a.counts;
-    m.new_lens = a.new_lens;
-    return launch_kernel(kvx_commit_kernel, commit_groups(c, num_layers), kWg, stream, m);
+    CommitArgs a = given;
+    a.lg_lanes = row_lanes(int64_t(a.c.hd) * a.c.row_bytes);
+    return launch_kernel(kvx_commit_kernel, commit_groups(a.c, a.num_layers), kWg, stream, a);
 }
 
 }  // namespace kvx

@@ -125,7 +125,9 @@ class Engine:
         return out
 
     def evict(self):
-        """Requests over the budget keep BUDGET slots of every layer and head."""
+        """Requests over the budget keep BUDGET slots of every layer and head.  The kept
+        keys stay turned by their old positions; a window or a bias (this engine has
+        none) would go by slots from here on."""
         kept = torch.empty((LAYERS, self.requests, HEADS, BUDGET), dtype=torch.int32, device="cuda")
         new_lens = torch.empty(self.requests, dtype=torch.int32, device="cuda")
         K.kvx_evict(self.view, 0, LAYERS, int32(self.lens), max(self.lens), BUDGET, SINK, RECENT, self.weights,

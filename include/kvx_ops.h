@@ -15,7 +15,9 @@
  * [layer][k/v][num_blocks][block_size][Hd].  Slot j of request r is slot
  * j % block_size of page block_table[r * bt_stride + j / block_size].  A page id
  * outside [0, num_blocks) names no page: its slots are not seen by attention,
- * weigh nothing, and are neither moved nor written.
+ * weigh nothing, and are neither moved nor written.  Requests may name the same page
+ * where they only read it; slots that kvx_append writes, or that kvx_evict and
+ * kvx_commit move, lie in pages of one request alone.
  *
  * A batch holds the new tokens of the requests, request r's at tokens
  * token_starts[r] .. token_starts[r + 1] - 1 of the flat token axis, n_r of
@@ -85,7 +87,11 @@ typedef struct {
  *   slopes: x -= slopes[query head] * |position of the token - position of the slot|.
  * Slot j is visible to token i of request r when j < prefix[r], or when
  *   (j < C_r, or the tree says so) and, for window > 0,
- *   position of the token - position of the slot < window. */
+ *   position of the token - position of the slot < window.
+ * A slot in use has its own number as its position, also after kvx_evict has moved
+ * another token's row there (each head its own): over an evicted request a bias and a
+ * window go by slots, and positions counted in slots (kvx_batch.positions NULL)
+ * belong to them.  What lies further back than the tokens between is then nearer. */
 typedef struct {
     float scale;
     float softcap;              /* 0: none */
@@ -119,7 +125,9 @@ typedef struct {
  *            q_heads 0: keys and values only.
  * Values are turned in fp32 and rounded once: q to dtype, k and v to the
  * cache's type (to nearest even; an 8-bit cache takes the casts of kvx.h, its
- * scale from the fp32 row).  Tokens whose slot has no page write no row.
+ * scale from the fp32 row).  Tokens whose slot has no page write no row.  A 16-bit
+ * cache may have the other 16-bit type than k and v; kvx_attend and kvx_weigh then
+ * take queries of the cache's type.
  * KVX_EINVAL: NULL or misaligned pointers, sizes out of the ranges above, layer
  * outside the cache.  KVX_EUNSUPPORTED: head_dim above 256. */
 kvx_status kvx_append(const kvx_cache *cache, const kvx_batch *batch, const kvx_rope *rope,

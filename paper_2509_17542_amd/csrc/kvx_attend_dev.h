@@ -93,6 +93,15 @@ __device__ __forceinline__ uint32_t pair16(uint32_t key0, uint32_t key1)
     return __builtin_amdgcn_perm(key1, key0, kHi ? 0x07060302u : 0x05040100u);
 }
 
+// A value that the compiler does not know: what follows from it is formed where it is
+// used.  After a walk over the slots the lane's place is taken from one, since what
+// is formed ahead and kept until then costs the walk registers.
+__device__ __forceinline__ int hidden(int x)
+{
+    __asm__ volatile("" : "+v"(x));
+    return x;
+}
+
 // ---- non-finite values ---------------------------------------------------------
 //
 // A weight of 0 does not hide an infinity from a matrix product (0 x inf is
@@ -185,7 +194,12 @@ struct Had {
     uint64_t bits[3][(kN + 63) / 64] = {};
     __device__ __forceinline__ void add(int at, float count, int kind)
     {
-        bits[kind - 1][kN <= 64 ? 0 : at >> 6] |= uint64_t(count > 0.0f) << (at & 63);
+        // no index by kind or place: the bits stay in registers
+        const uint64_t bit = uint64_t(count > 0.0f) << (at & 63);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int w = 0; w < (kN + 63) / 64; ++w) bits[k][w] |= kind == k + 1 && at >> 6 == w ? bit : 0;
     }
     // what sum `at` is, which the products say is `o`
     __device__ __forceinline__ float of(int at, float o) const

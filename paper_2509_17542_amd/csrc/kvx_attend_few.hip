@@ -437,11 +437,7 @@ __global__ void __launch_bounds__(kWg, (kWavesPerSimd<kCodes, DP, RT>)) kvx_atte
     for (int rt = 0; rt < RT; ++rt) special |= __any(live[rt] && any_endless<4, DT>(o[rt])) != 0;
     if (__builtin_expect(special, 0)) {
         // the tiles again, an element of V's rows at a time: which sums had infinities or NaN
-        // (the lane's number hidden from the compiler, and what follows from it formed anew: values
-        // kept for this path cost the first walk registers)
-        int hidden = lane;
-        __asm__ volatile("" : "+v"(hidden));
-        const int n16 = hidden & 15, g = hidden >> 4;
+        const int place = hidden(lane), n16 = place & 15, g = place >> 4;
         Had<4 * DT> had[RT];
 #pragma unroll 1
         for (v = v0 + wave * kTile; v < v1; v += kWaves * kTile) {

@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     __shared__ __attribute__((aligned(16))) float s_ks[k8 ? 2 * kWg : 1];
     __shared__ __attribute__((aligned(16))) float s_vs[k8 ? 2 * kWg : 1];
     __shared__ uint64_t s_valid[S::kRing];
-    __shared__ int s_special, s_some[2][NW];
+    __shared__ int s_special;
 
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, half = lane >> 5;
@@ -241,9 +241,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         }
         return w;
     };
-    // kind 0: K, and V with its values that are not finite as 0 where not every row sees the
-    // tile whole; 1 to 3: ones where V (8-bit: a code times its slot's scale) is +inf, -inf, NaN
-    auto store = [&](int t, uint64_t valid, int kind) {
+    // K, and V with its values that are not finite as 0 where not every row sees the tile whole
+    auto store = [&](int t, uint64_t valid) {
         char* const ks = s_k[t & 1];
         char* const vs = s_v[t & 1];
         const bool whole = whole_tile(t, valid);
@@ -261,7 +260,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             if (S::kVUnits % kWg && unit >= S::kVUnits) break;
             const int kg = unit / (DP / 4), d = unit % (DP / 4) * 4;
             char* const out = vs + d * S::kVRow + (kg ^ ((d >> 4) & 3)) * 16;
-            if (whole && kind == 0) {
+            if (whole) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4*>(out + e * S::kVRow) = column(vr[i], e);
             } else {
@@ -274,18 +273,11 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     found |= nonfinite<kBf16, kCodes>(x[e].x);
                     if constexpr (!k8) found |= nonfinite<kBf16, kCodes>(x[e].y);
                 }
-                if (found && kind == 0) s_special = 1;
+                if (found) s_special = 1;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    u32x4 w = column(x, e);
-                    if (k8 && kind != 0) {
-                        const float* const at = s_vs + (t & (S::kRing - 1)) * KT + first;
-#pragma unroll
-                        for (int p = 0; p < 4; ++p)
-                            w[p] = times2<kBf16>(w[p], scale_kind(at[2 * (p & 1) + 8 * (p >> 1)]),
-                                                 scale_kind(at[2 * (p & 1) + 8 * (p >> 1) + 1]));
-                    }
-                    *reinterpret_cast<u32x4*>(out + e * S::kVRow) = kind == 0 && !found ? w : classify8<kBf16>(w, kind);
+                    const u32x4 w = column(x, e);
+                    *reinterpret_cast<u32x4*>(out + e * S::kVRow) = found ? classify8<kBf16>(w, 0) : w;
                     __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
                 }
             }
@@ -500,7 +492,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         for (int t = 0; t < tiles; ++t) {
             const int batch = t / S::kBatch, phase = t % S::kBatch;
             const int next = min(t + 1, tiles - 1);  // the last again: nothing waits for it
-            store(t, valid, 0);
+            store(t, valid);
             if (phase == 1) note_scales(batch + 1);
             places(next);
             const uint64_t next_valid = valid_of(next);
@@ -514,8 +506,12 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
         if (live && any_endless<16, DTB>(o)) s_special = 1;
         __syncthreads();
         if (__builtin_expect(s_special, 0)) {
-            // the tiles again: which sums had infinities or NaN
+            // the tiles again, an element of V's rows at a time: which sums had infinities or NaN
+            const int place = hidden(lane), n32 = place & 31, half = place >> 5, row = row0 + wave * 32 + n32;
+            const int i = int(fast_div(uint32_t(row < rows ? row : row0), a.div_group));
+            const int pos = a.b.positions ? a.b.positions[rq.first + i] : rq.ctx + i;
             Had<16 * DTB> had;
+#pragma unroll 1
             for (int t = 0; t < tiles; ++t) {
                 if (t % S::kBatch == 0) {
                     __syncthreads();
@@ -525,57 +521,45 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     __syncthreads();
                 }
                 valid = valid_of(t);
-                places(t);
-                load();
-                bool some = false;
+                const uint64_t mine =
+                    row < rows ? seen_of(a, rq, r, i, pos, rg.slot(tile_at(t)), valid) >> (4 * half) : 0;
+                const int first = (t & (S::kRing - 1)) * KT;
+#pragma unroll 1
+                for (int t2 = 0; t2 < DTB; ++t2) {
+                    const int byte = (32 * t2 + n32) * S::kEl, at = byte < a.c.row_bytes ? byte : 0;
+#pragma unroll 1
+                    for (int e = 0; e < 2 * ST; ++e) {
+                        u32x4 f = {0, 0, 0, 0}, seen;
+                        uint32_t some = 0;
 #pragma unroll
-                for (int i = 0; i < S::kVPer; ++i) {
-                    const int kg = min((tid + i * kWg) / (DP / 4), KT / 8 - 1), first = (kg >> 1) * 16 + (kg & 1) * 4;
+                        for (int w = 0; w < 4; ++w) {
+                            const uint32_t two = uint32_t(mine >> (16 * e + 8 * (w >> 1) + 2 * (w & 1))) & 3u;
+                            seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int slot = first + (e & 3) + (e >> 2) * 8;
-                        if (!(valid >> slot & 1)) continue;
-                        some |= nonfinite<kBf16, kCodes>(vr[i][e].x) != 0;
-                        if constexpr (!k8) some |= nonfinite<kBf16, kCodes>(vr[i][e].y) != 0;
-                        if constexpr (k8)
-                            some |= !(__builtin_fabsf(s_vs[(t & (S::kRing - 1)) * KT + slot]) < INFINITY);
-                    }
-                }
-                const bool some_here = __any(some) != 0;
-                if (lane == 0) s_some[t & 1][wave] = some_here;
-                __syncthreads();
-                some = false;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) some |= s_some[t & 1][w] != 0;
-                if (!some) continue;
-                const uint64_t mine = live ? seen_by_me(t, valid) : 0;
-                for (int kind = 1; kind <= 3; ++kind) {
-                    places(t);
-                    load();
-                    store(t, valid, kind);
-                    __syncthreads();
-                    const char* const vl = s_v[t & 1] + n32 * S::kVRow + (half ^ (n32 >> 4)) * 16;
-#pragma unroll
-                    for (int t2 = 0; t2 < DTB; ++t2) {
-                        f32x16 count;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) count[i] = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < 2 * ST; ++e) {
-                            u32x4 seen;
-#pragma unroll
-                            for (int w = 0; w < 4; ++w) {
-                                const uint32_t two = uint32_t(mine >> (16 * e + 8 * (w >> 1) + 2 * (w & 1))) & 3u;
-                                seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
+                            for (int s = 0; s < 2; ++s) {
+                                const int slot = 16 * e + 8 * (w >> 1) + 4 * half + 2 * (w & 1) + s;
+                                const char* const from = vb + s_off[first + slot] + at;
+                                uint32_t x;
+                                if constexpr (k8)
+                                    x = times2<kBf16>(widen2<kBf16, kCodes, false>(*reinterpret_cast<const uint8_t*>(from)),
+                                                      scale_kind(s_vs[first + slot]), 0.0f) & 0xFFFFu;
+                                else
+                                    x = *reinterpret_cast<const uint16_t*>(from);
+                                f[w] |= (valid >> slot & 1 ? x : 0u) << (16 * s);
                             }
-                            count = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + (e >> 1) * 64 + ((e ^ t2) & 1) * 32),
-                                                  seen, count);
+                            some |= nonfinite<kBf16, kCodes16>(f[w]);
                         }
+                        if (!__any(some != 0)) continue;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) had.add(16 * t2 + i, count[i], kind);
-                        __builtin_amdgcn_sched_barrier(0);
+                        for (int kind = 1; kind <= 3; ++kind) {
+                            f32x16 count;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) count[i] = 0.0f;
+                            count = mfma32<kBf16>(classify8<kBf16>(f, kind), seen, count);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) had.add(16 * t2 + i, count[i], kind);
+                        }
                     }
-                    __syncthreads();
                 }
             }
 #pragma unroll
@@ -588,41 +572,46 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     l += __shfl_xor(l, 32);
     if constexpr (kLift) l *= 65536.0f;              // 2^kLiftShift
     const float back = kLift ? unlifted(lift) : 1.0f;
-    if (!live) return;
-    const int64_t at = token * a.q_heads + head;
-    if (a.splits > 1) {
-        const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
-        if (half == 0) {
-            a.part_ml[2 * (split * pairs + at)] = reference_of(m, l);
-            a.part_ml[2 * (split * pairs + at) + 1] = l;
+    {
+        // the row's place, formed anew
+        const int place = hidden(lane), half = place >> 5, row = row0 + wave * 32 + (place & 31);
+        if (row >= rows) return;
+        const int i = int(fast_div(uint32_t(row), a.div_group)), head = h * G + (row - i * G);
+        const int64_t token = rq.first + i, at = token * a.q_heads + head;
+        if (a.splits > 1) {
+            const int64_t pairs = int64_t(a.b.total_tokens) * a.q_heads;
+            if (half == 0) {
+                a.part_ml[2 * (split * pairs + at)] = reference_of(m, l);
+                a.part_ml[2 * (split * pairs + at) + 1] = l;
+            }
+            if (l == 0.0f) return;
+            float* const out = a.part_o + (split * pairs + at) * D;
+#pragma unroll
+            for (int t = 0; t < DTB; ++t)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int d = 32 * t + 8 * b + 4 * half;
+                    f32x4 x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = kLift ? o[t][4 * b + i] * back : o[t][4 * b + i];
+                    if (d < D) *reinterpret_cast<f32x4*>(out + d) = x;
+                }
+        } else {
+            const float inv = l == 0.0f ? 0.0f : back / l;
+            uint16_t* const out = a.out + token * a.out_stride + int64_t(head) * D;
+#pragma unroll
+            for (int t = 0; t < DTB; ++t)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int d = 32 * t + 8 * b + 4 * half;
+                    const uint2 w = l == 0.0f ? make_uint2(0, 0)
+                                              : make_uint2(pack2<kBf16>(o[t][4 * b] * inv, o[t][4 * b + 1] * inv),
+                                                           pack2<kBf16>(o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv));
+                    if (d < D) *reinterpret_cast<uint2*>(out + d) = w;
+                }
+            if (a.lse && half == 0)
+                a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kShift<kBf16>) * kLn2;
         }
-        if (l == 0.0f) return;
-        float* const out = a.part_o + (split * pairs + at) * D;
-#pragma unroll
-        for (int t = 0; t < DTB; ++t)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int d = 32 * t + 8 * b + 4 * half;
-                f32x4 x;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = kLift ? o[t][4 * b + i] * back : o[t][4 * b + i];
-                if (d < D) *reinterpret_cast<f32x4*>(out + d) = x;
-            }
-    } else {
-        const float inv = l == 0.0f ? 0.0f : back / l;
-        uint16_t* const out = a.out + token * a.out_stride + int64_t(head) * D;
-#pragma unroll
-        for (int t = 0; t < DTB; ++t)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int d = 32 * t + 8 * b + 4 * half;
-                const uint2 w = l == 0.0f ? make_uint2(0, 0)
-                                          : make_uint2(pack2<kBf16>(o[t][4 * b] * inv, o[t][4 * b + 1] * inv),
-                                                       pack2<kBf16>(o[t][4 * b + 2] * inv, o[t][4 * b + 3] * inv));
-                if (d < D) *reinterpret_cast<uint2*>(out + d) = w;
-            }
-        if (a.lse && half == 0)
-            a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kShift<kBf16>) * kLn2;
     }
 }
 

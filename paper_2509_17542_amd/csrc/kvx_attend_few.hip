@@ -16,7 +16,7 @@
 // Where a slot's row lies is looked up once per chunk into LDS.
 //
 // 64 requests of 512..8192 slots, one token each (8 KV heads, 128 elements, bf16,
-// 1.1 GB) take 214 us, 5.1 TB/s, and 5 for the join; one token over 255 slots 5.6.
+// 1.1 GB) take 214 us, 5.1 TB/s, and 5 for the join; one token over 255 slots 5.7.
 // A plain stream of 256-byte pieces at 2 KB strides reads 6.4 TB/s, so what is left
 // is the chunks' ends: places looked up before the first row, sums written after
 // the last, and idle chunks of requests shorter than the longest.

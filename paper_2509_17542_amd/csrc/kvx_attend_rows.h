@@ -18,17 +18,21 @@
 // Bound by the matrix instructions and the exponentials between them: 1024
 // matrix cycles of a SIMD for a tile of 64 slots and 128 rows of 128 elements,
 // 210 (plain scores) to 360 (capped, 8-bit codes) vector instructions, and the
-// wait of one for the other.  8 requests of 2048 tokens on 8192 slots run at 775
-// TFLOP/s in fp16 and 817 in bf16 (a library's large product of that type alone:
+// wait of one for the other; and by LDS, out of which each wave reads all of a tile:
+// for chunks of many tokens it is busy 39% of the cycles (30% of these conflicts),
+// the matrix pipes 32%.  8 requests of 2048 tokens on 8192 slots run at 807 to 835
+// TFLOP/s in fp16 and 850 in bf16 (a library's large product of that type alone:
 // 1342, 1410); three chunks of 1024..2048 tokens with a bias, a window and a
-// prefix, whose edges cost partial tiles, in 0.65 to 0.71 ms, 710 to 765 TFLOP/s; 16
+// prefix, whose edges cost partial tiles, in 0.64 to 0.69 ms, 730 to 780 TFLOP/s; 16
 // trees of 16..64 nodes over an fp8 cache of 2048..16384 slots, capped scores, in
-// 320 to 375 us, 25 of them the join.
+// 318 to 325 us, 24 of them the join.  These are times of a card in use: its first
+// milliseconds of such work after a pause run at about 2 GHz, not 2.4 (0.72 ms and 380
+// us).
 //
 // 128 rows share a tile, 64 slots of it; up to 64 rows have half the waves, so that
 // none only stages, and 32 slots, so that twice as many workgroups fit a CU's LDS
 // (trees of 9..16 nodes, 36..64 rows, over the same fp8 cache: 165 us, 190 in workgroups of
-// 128; 64 such over a bf16 cache of 512..8192 slots 303, 340).
+// 128; 64 such over a bf16 cache of 512..8192 slots 303, 340; in longer runs now 154 and 293).
 // A weight (8-bit codes: times its slot's scale) goes to 16 bits for the product with
 // V; its rounding is the type's own half unit in the last place, relative (a second
 // product with what it left would cost the three chunks 816 us, 657 without, and the 16

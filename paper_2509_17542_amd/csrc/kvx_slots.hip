@@ -69,8 +69,8 @@ __device__ __forceinline__ uint4 narrow(const float (&x)[8])
 // (interleaved) or is read again, out of the cache (halves; pairs that do not fill
 // whole lanes element by element).  Bound by memory for prompts and by its chain
 // of lookups for single tokens.  Prompts of 500..3000 tokens, three axes, into an
-// fp8 cache (250 MB) take 53 us, 4.7 TB/s, and into a bf16 one 60; with four tokens
-// a workgroup 59 and 70.
+// fp8 cache (250 MB) take 61 us, 4.1 TB/s, on buffers that change from call to call;
+// on the same ones 53, and 60 into a bf16 cache, with four tokens a workgroup 59 and 70.
 template <bool kBf16, int kCache, int kPairing>
 __global__ void __launch_bounds__(kWg) kvx_append_kernel(const AppendArgs a)
 {
@@ -367,7 +367,8 @@ __device__ __forceinline__ void arrived(Held& v)
 // are read non-temporal (kOnce): a prompt of 16001 slots cut to 2048 in 32 layers
 // takes 127 us so and 148 without, both with a slower selection (now 117, the move
 // 93 of it, 5.8 TB/s; bf16, rows of 256 bytes); an fp8 batch, rows of 128 bytes, 99
-// and 91 (the move 78, 5.3 TB/s).
+// and 91 (the move 78, 5.3 TB/s).  All of this on the same buffers in every call, what
+// the last one wrote still in the memory-side cache; on changing ones 143 and 114.
 template <bool kOnce>
 __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
 {
@@ -547,7 +548,7 @@ int row_lanes(int64_t bytes)
 }
 
 // long requests take more threads, the passes over the weights being a chain (16001 slots, 32
-// layers: 119 us, 143 with 256 threads); short ones do not fill them (1100..1160 slots, 24
+// layers, the same buffers in every call: 119 us, 143 with 256 threads); short ones do not fill them (1100..1160 slots, 24
 // requests in 4 layers: 90 us, 107 with 1024 threads)
 int select_threads(int max_len) { return max_len > 4096 ? 1024 : kWg; }
 

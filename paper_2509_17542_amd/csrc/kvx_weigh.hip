@@ -10,8 +10,8 @@
 // stay in LDS leave registers for four (32 requests of 512..4096 slots, e5m2: 24
 // us; 30 with 64 keys in registers).  For more it is bound by the matrix
 // instructions and the exponentials, and 64 keys in registers serve all rows
-// (the last 32 tokens of two prompts of 16000..32000 slots, 128 rows: 45 us,
-// 2.3 TB/s and 285 TFLOP/s; 68 the other way).  No two
+// (the last 32 tokens of two prompts of 16000..32000 slots, 128 rows: 42 us,
+// 2.5 TB/s and 304 TFLOP/s; in short runs 45, and 68 the other way).  No two
 // waves write the same slot, so nothing is added atomically.
 #include <hip/hip_runtime.h>
 

@@ -12,7 +12,8 @@
  *
  * The cache is the one that kvx_unpack and kvx_repack write:
  * [layer][k/v][num_blocks][block_size][Hd][D] and, for 8-bit codes, fp32 scales
- * [layer][k/v][num_blocks][block_size][Hd].  Slot j of request r is slot
+ * [layer][k/v][num_blocks][block_size][Hd]; or one of 4 bits, which kvx_append fills
+ * (KVX_FP4_E2M1).  Slot j of request r is slot
  * j % block_size of page block_table[r * bt_stride + j / block_size].  A page id
  * outside [0, num_blocks) names no page: its slots are not seen by attention,
  * weigh nothing, and are neither moved nor written.  Requests may name the same page
@@ -48,21 +49,33 @@ extern "C" {
 
 #define KVX_OPS_VERSION 1
 
+/* A cache's element type beside those of kvx_dtype: e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4,
+ * 6 and their negatives; the sign is bit 3), two a byte, the element of the even
+ * number in the lower bits, [layer][k/v][num_blocks][block_size][Hd][D / 2], and a
+ * scale byte b for every 32 elements of a row,
+ * [layer][k/v][num_blocks][block_size][Hd][D / 32]: an element is its code's value times
+ * 2^(b - 127), and NaN where b is above 252.  kvx_append takes the smallest scale with
+ * |x| <= 7 scale in the group, so that no element is off by more than half a step of its
+ * size, cut to 2^-126 .. 2^125, and divides, rounds to nearest even and cuts at 6; a group
+ * with an element that is not finite becomes NaN. */
+#define KVX_FP4_E2M1 5
+
 int32_t kvx_ops_version(void);
 
 /* A decode rank's paged cache and the block table of the requests at hand. */
 typedef struct {
     int32_t num_layers;
     int32_t num_kv_heads;       /* Hd: KV heads of this rank */
-    int32_t head_dim;           /* D: a multiple of 8 (16-bit) or 16 (8-bit), at most 256 */
-    int32_t dtype;              /* kvx_dtype of the cache */
+    int32_t head_dim;           /* D: a multiple of 8 (16-bit), 16 (8-bit) or 32 (4-bit), at most 256 */
+    int32_t dtype;              /* kvx_dtype of the cache, or KVX_FP4_E2M1 */
     int32_t block_size;         /* slots per page */
     int32_t num_requests;       /* rows of the block table */
     int32_t bt_stride;          /* entries per row */
     int32_t reserved;
     int64_t num_blocks;         /* pages per (layer, k/v) plane */
     void *cache;                /* device, 16-byte aligned */
-    float *scales;              /* device, non-NULL if and only if dtype is 8-bit */
+    float *scales;              /* device, non-NULL if and only if dtype is 8-bit or 4-bit (the
+                                 * scale bytes then, cast) */
     const int32_t *block_table; /* device [num_requests][bt_stride] */
 } kvx_cache;
 

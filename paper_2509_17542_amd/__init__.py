@@ -32,6 +32,7 @@ if _lib.kvx_abi_version() != ABI_VERSION:
 
 OK, EINVAL, EUNSUPPORTED, ENOMEM, EDEVICE = 0, -1, -2, -3, -4
 FP16, BF16, E4M3FN, E5M2 = 1, 2, 3, 4
+E2M1 = 5                       # a cache's only, see kvx_ops.h
 THD, HTD, PAGED = 0, 1, 2
 _STATUS = {0: "KVX_OK", -1: "KVX_EINVAL", -2: "KVX_EUNSUPPORTED", -3: "KVX_ENOMEM",
            -4: "KVX_EDEVICE"}
@@ -513,17 +514,26 @@ def kvx_pd_evaluate(problem: kvx_pd_problem, side: int, dp: int, tp: int, pp: in
 
 
 # The decode operators over the cache (include/kvx_ops.h) are bound in
-# operators.py, which is read at the first use of one of its names.
+# operators.py, what include/kvx_serve.h adds in serving.py: each is read at the
+# first use of one of its names.
 _OPERATOR_NAMES = frozenset((
     "OPERATORS", "OPS_VERSION", "kvx_append", "kvx_attend", "kvx_attend_workspace", "kvx_batch",
     "kvx_cache", "kvx_commit", "kvx_evict", "kvx_ops_version", "kvx_rope", "kvx_scores",
     "kvx_weigh", "make_batch", "make_cache", "make_rope", "make_scores"))
+_SERVING_NAMES = frozenset((
+    "FP32", "SERVE_VERSION", "SERVING", "kvx_drafts", "kvx_fetch", "kvx_serve_version", "kvx_verify",
+    "kvx_verify_workspace", "make_drafts"))
 
 
 def __getattr__(name):
-    if name not in _OPERATOR_NAMES:
+    if name in _OPERATOR_NAMES:
+        from . import operators as module
+        names = _OPERATOR_NAMES
+    elif name in _SERVING_NAMES:
+        from . import serving as module
+        names = _SERVING_NAMES
+    else:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-    from . import operators
-    for n in _OPERATOR_NAMES:
-        globals()[n] = getattr(operators, n)
+    for n in names:
+        globals()[n] = getattr(module, n)
     return globals()[name]

@@ -1,4 +1,5 @@
-// Host side of the decode operators (kvx_ops.h): argument checks and launches.
+// Host side of the decode operators (kvx_ops.h, kvx_fetch of kvx_serve.h): argument checks and
+// launches.
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
@@ -12,6 +13,8 @@ namespace {
 using kvx::fail;
 
 bool is_fp8(int dt) { return dt == KVX_FP8_E4M3FN || dt == KVX_FP8_E5M2; }
+
+bool is_fp4(int dt) { return dt == KVX_FP4_E2M1; }
 
 bool is_16bit(int dt) { return dt == KVX_FP16 || dt == KVX_BF16; }
 
@@ -28,10 +31,12 @@ kvx_status check_shape(const kvx_cache* c)
     if (c->num_layers < 1 || c->num_kv_heads < 1 || c->head_dim < 1 || c->block_size < 1 ||
         c->num_blocks < 1)
         return fail(KVX_EINVAL, "a cache's layers, heads, head_dim, block_size and num_blocks must be >= 1");
-    if (!is_fp8(c->dtype) && !is_16bit(c->dtype))
+    if (!is_fp8(c->dtype) && !is_16bit(c->dtype) && !is_fp4(c->dtype))
         return fail(KVX_EINVAL, "unknown cache dtype %d", c->dtype);
     if (c->num_requests < 0 || c->bt_stride < 0)
         return fail(KVX_EINVAL, "num_requests and bt_stride must be >= 0");
+    if (is_fp4(c->dtype) && c->head_dim % 32)
+        return fail(KVX_EINVAL, "head_dim %d: rows of a 4-bit cache must be whole groups of 32", c->head_dim);
     if (c->head_dim % (is_fp8(c->dtype) ? 16 : 8))
         return fail(KVX_EINVAL, "head_dim %d: rows must be whole 16-byte vectors", c->head_dim);
     if (c->head_dim > 256) return fail(KVX_EUNSUPPORTED, "head_dim %d above 256", c->head_dim);
@@ -48,8 +53,8 @@ kvx_status check_buffers(const kvx_cache& c)
 {
     if (!c.cache || !c.block_table) return fail(KVX_EINVAL, "NULL cache or block table");
     if (!aligned16(c.cache)) return fail(KVX_EINVAL, "the cache must be 16-byte aligned");
-    if (is_fp8(c.dtype) != (c.scales != nullptr))
-        return fail(KVX_EINVAL, "scales must be given exactly for an 8-bit cache");
+    if ((is_fp8(c.dtype) || is_fp4(c.dtype)) != (c.scales != nullptr))
+        return fail(KVX_EINVAL, "scales must be given exactly for an 8-bit or a 4-bit cache");
     return KVX_OK;
 }
 
@@ -94,12 +99,16 @@ kvx_status check_rows(const char* what, const void* p, int64_t stride, int64_t w
 kvx::CacheArgs cache_args(const kvx_cache& c, int layer0)
 {
     kvx::CacheArgs a = {};
-    const int esz = is_fp8(c.dtype) ? 1 : 2;
-    a.row_bytes = c.head_dim * esz;
+    const bool four = is_fp4(c.dtype);
+    a.row_bytes = four ? c.head_dim / 2 : c.head_dim * (is_fp8(c.dtype) ? 1 : 2);
+    a.row_groups = four ? c.head_dim / 32 : 0;
     a.plane_scales = c.num_blocks * c.block_size * c.num_kv_heads;
     a.plane_bytes = a.plane_scales * a.row_bytes;
     a.base = static_cast<char*>(c.cache) + 2 * int64_t(layer0) * a.plane_bytes;
-    a.scales = c.scales ? c.scales + 2 * int64_t(layer0) * a.plane_scales : nullptr;
+    if (four)
+        a.groups = reinterpret_cast<uint8_t*>(c.scales) + 2 * int64_t(layer0) * a.plane_scales * a.row_groups;
+    else if (c.scales)
+        a.scales = c.scales + 2 * int64_t(layer0) * a.plane_scales;
     a.table = c.block_table;
     a.num_blocks = c.num_blocks;
     a.bt_stride = c.bt_stride;
@@ -166,7 +175,7 @@ kvx_status check_scores(const kvx_cache* c, const kvx_batch* b, const kvx_scores
         return fail(KVX_EINVAL, "softcap must be finite and >= 0");
     if (s->window < 0) return fail(KVX_EINVAL, "window must be >= 0");
     if (!is_16bit(dtype)) return fail(KVX_EINVAL, "q must be KVX_FP16 or KVX_BF16, not %d", dtype);
-    if (!is_fp8(c->dtype) && c->dtype != dtype)
+    if (is_16bit(c->dtype) && c->dtype != dtype)
         return fail(KVX_EUNSUPPORTED, "a 16-bit cache must have the type of q");
     if (q_heads < 1 || q_heads % c->num_kv_heads)
         return fail(KVX_EINVAL, "q_heads %d is not a multiple of %d KV heads", q_heads,
@@ -257,6 +266,32 @@ extern "C" kvx_status kvx_append(const kvx_cache* c, const kvx_batch* b, const k
     return launched(kvx::launch_append(a, dtype, c->dtype, stream));
 }
 
+extern "C" int32_t kvx_serve_version(void) { return KVX_SERVE_VERSION; }
+
+extern "C" kvx_status kvx_fetch(const kvx_cache* c, const kvx_batch* b, int32_t layer, int32_t dtype,
+                                void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream)
+{
+    KVX_TRY(check_shape(c));
+    KVX_TRY(check_batch(*c, b));
+    KVX_TRY(check_layers(*c, layer, 1));
+    if (!is_16bit(dtype)) return fail(KVX_EINVAL, "k and v must be KVX_FP16 or KVX_BF16, not %d", dtype);
+    if (b->total_tokens == 0 || c->num_requests == 0) return KVX_OK;
+    KVX_TRY(check_buffers(*c));
+    const int64_t width = int64_t(c->num_kv_heads) * c->head_dim;
+    KVX_TRY(check_rows("k", k, k_stride, width));
+    KVX_TRY(check_rows("v", v, v_stride, width));
+    KVX_TRY(check_threads(kvx::fetch_threads(b->total_tokens)));
+    KVX_TRY(need_device());
+    kvx::FetchArgs a = {};
+    a.c = cache_args(*c, layer);
+    a.b = batch_args(*b);
+    a.k = static_cast<uint16_t*>(k);
+    a.v = static_cast<uint16_t*>(v);
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    return launched(kvx::launch_fetch(a, dtype, c->dtype, stream));
+}
+
 extern "C" kvx_status kvx_attend_workspace(const kvx_cache* c, const kvx_batch* b, int32_t q_heads,
                                            uint64_t* bytes)
 {
@@ -279,6 +314,7 @@ extern "C" kvx_status kvx_attend(const kvx_cache* c, const kvx_batch* b, const k
     KVX_TRY(check_scores(c, b, s, layer, dtype, q_heads, &idle));
     if (idle) return KVX_OK;
     KVX_TRY(check_buffers(*c));
+    if (is_fp4(c->dtype)) return fail(KVX_EUNSUPPORTED, "kvx_attend over a 4-bit cache");
     KVX_TRY(check_rows("q", q, q_stride, int64_t(q_heads) * c->head_dim));
     KVX_TRY(check_rows("out", out, out_stride, int64_t(q_heads) * c->head_dim));
     const uint64_t need = kvx::attend_workspace(*c, *b, q_heads);
@@ -310,6 +346,7 @@ extern "C" kvx_status kvx_weigh(const kvx_cache* c, const kvx_batch* b, const kv
     if (!lse || !weights) return fail(KVX_EINVAL, "NULL lse or weights");
     if (w_stride < b->max_context)
         return fail(KVX_EINVAL, "w_stride %lld below max_context %d", (long long)w_stride, b->max_context);
+    if (is_fp4(c->dtype)) return fail(KVX_EUNSUPPORTED, "kvx_weigh over a 4-bit cache");
     KVX_TRY(check_threads(kvx::weigh_threads(*c, *b, q_heads)));
     KVX_TRY(need_device());
     kvx::AttendArgs a = attend_args(*c, *b, *s, layer, q_heads);

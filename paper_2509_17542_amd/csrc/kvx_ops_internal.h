@@ -1,12 +1,13 @@
 // Internal declarations shared by the host side of the decode operators
-// (kvx_ops.cpp) and their kernels: kvx_slots.hip (append, evict, commit),
-// kvx_attend.hip with kvx_attend_few.hip and kvx_attend_rows*, kvx_weigh.hip.
+// (kvx_ops.cpp, kvx_verify.cpp) and their kernels: kvx_slots.hip (append, fetch,
+// evict, commit), kvx_attend.hip with kvx_attend_few.hip and kvx_attend_rows*,
+// kvx_weigh.hip, kvx_verify.hip.
 #pragma once
 
 #include <cstdint>
 
 #include "kvx_internal.h"
-#include "kvx_ops.h"
+#include "kvx_serve.h"
 
 namespace kvx {
 
@@ -14,19 +15,20 @@ namespace kvx {
 // of one (layer, k/v): [num_blocks][block_size][hd][dim].
 struct CacheArgs {
     char* base;                  // plane (layer0, k)
-    float* scales;               // its scales, NULL for 16-bit elements
+    float* scales;               // its scales, NULL but for 8-bit elements
+    uint8_t* groups;             // its scale bytes, NULL but for 4-bit elements
     const int32_t* table;
     int64_t plane_bytes;         // bytes between planes
-    int64_t plane_scales;        // scales between planes
+    int64_t plane_scales;        // scales between planes (4-bit elements: x row_groups bytes)
     int64_t num_blocks;
     int32_t bt_stride;
     int32_t block_size;
     int32_t hd;
     int32_t dim;
     int32_t row_bytes;           // dim x element size
+    int32_t row_groups;          // scale bytes of a row: dim / 32 for 4-bit elements, else 0
     int32_t row_slots;           // slots of a block-table row: bt_stride x block_size, cut to int32
     int32_t num_requests;
-    int32_t pad;
     FastDiv div_bs;              // by block_size
 };
 
@@ -56,6 +58,14 @@ struct AppendArgs {
     int32_t interleaved;
     int32_t sec_end[4];          // pairs below sec_end[a] belong to an axis <= a
     int32_t lg_row;              // log2 of the lanes per head: a power of two >= dim / 8
+};
+
+struct FetchArgs {
+    CacheArgs c;
+    BatchArgs b;
+    uint16_t* k;
+    uint16_t* v;
+    int64_t k_stride, v_stride;
 };
 
 struct EvictArgs {
@@ -135,6 +145,7 @@ int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, void* strea
 // The threads of a call's largest launch, workgroups times their size: HIP takes
 // fewer than 2^32.
 double append_threads(int32_t tokens);
+double fetch_threads(int32_t tokens);
 double evict_threads(const CacheArgs& c, int num_layers, int max_len);
 double commit_threads(const CacheArgs& c, int num_layers);
 double attend_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads, const AttendPlan& p);
@@ -142,6 +153,7 @@ double weigh_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
 
 // Each enqueues its kernels on `stream` and returns a hipError_t value.
 int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream);
+int launch_fetch(const FetchArgs& a, int dtype, int cache_dtype, void* stream);
 int launch_evict(const EvictArgs& a, int num_layers, void* stream);
 int launch_commit(const CommitArgs& a, void* stream);
 int launch_attend(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype,

@@ -1,5 +1,5 @@
-// gfx950 kernels that write and move rows of the paged cache: kvx_append (the
-// new tokens' rows, with rotary positions), kvx_evict (selection by weight, then
+// gfx950 kernels that write, read back and move rows of the paged cache: kvx_append
+// (the new tokens' rows, with rotary positions), kvx_fetch, kvx_evict (selection by weight, then
 // the move of what stays, a head's rows at a time) and kvx_commit (the move of a
 // path's rows, all heads at a time).
 #include <hip/hip_runtime.h>
@@ -12,6 +12,8 @@ namespace kvx {
 namespace {
 
 constexpr int kWg = 256;
+
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
 // ---- append ------------------------------------------------------------------
 
@@ -39,6 +41,28 @@ __device__ __forceinline__ uint32_t code8(float x, float s)
     else
         code = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, c, 0, false)) & 0x7Fu;
     return sign | code;
+}
+
+// The scale byte of a group whose largest magnitude has the bits `most`: 2^(b - 127) is
+// the smallest with 7 of them not below it (adding what is missing from 1.75 to 2
+// carries into the exponent exactly above 1.75), cut to 1 .. 252; 255 for a group that
+// is not finite.
+__device__ __forceinline__ uint32_t group_scale(uint32_t most)
+{
+    if (most >= 0x7F800000u) return 255u;
+    return uint32_t(min(max(int((most + 0x1FFFFFu) >> 23) - 2, 1), 252));
+}
+
+// 8 values -> codes of 4 bits, x / 2^(b - 127) to nearest even, cut at 6.  The division is
+// by a power of two, so the codes are those of the values themselves.
+__device__ __forceinline__ uint32_t codes4(const float (&x)[8], uint32_t b)
+{
+    const float s = __uint_as_float(b << 23);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
 }
 
 enum Pairing : int { kHalves = 0, kInterleaved = 1, kAnyHalves = 2 };
@@ -155,6 +179,19 @@ __global__ void __launch_bounds__(kWg) kvx_append_kernel(const AppendArgs a)
         char* const dst = a.c.base + kv * a.c.plane_bytes + (row + head) * a.c.row_bytes;
         if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
             if (row >= 0 && in_row) *reinterpret_cast<uint4*>(dst + e0 * 2) = narrow<kCache == KVX_BF16>(x);
+        } else if constexpr (kCache == KVX_FP4_E2M1) {
+            // 4 lanes to a group; as bits a NaN is above all others
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+            m = max(m, uint32_t(__shfl_xor(int(m), 1)));
+            m = max(m, uint32_t(__shfl_xor(int(m), 2)));
+            const uint32_t b = group_scale(m), w = codes4(x, b);
+            if (row >= 0 && in_row) {
+                *reinterpret_cast<uint32_t*>(dst + (e0 >> 1)) = w;
+                if ((lane & 3) == 0)
+                    a.c.groups[(kv * a.c.plane_scales + row + head) * a.c.row_groups + (lane >> 2)] = uint8_t(b);
+            }
         } else {
             constexpr bool kE5 = kCache == KVX_FP8_E5M2;
             float m = 0.0f;
@@ -170,6 +207,86 @@ __global__ void __launch_bounds__(kWg) kvx_append_kernel(const AppendArgs a)
                 if (lane == 0) a.c.scales[kv * a.c.plane_scales + row + head] = s;
             }
         }
+    }
+}
+
+// ---- fetch -----------------------------------------------------------------------
+
+// 4 bytes of codes (8 elements of a group whose scale byte is b) -> values
+__device__ __forceinline__ void values4(uint32_t w, uint32_t b, float (&x)[8])
+{
+    const float s = __uint_as_float((b > 252u ? 255u : b) << 23);
+    const f32x2_t p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3)};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[e >> 1][e & 1];
+}
+
+// 4 codes of 8 bits -> values
+template <bool kE5>
+__device__ __forceinline__ void values8(uint32_t w, float* x)
+{
+    f32x2_t lo, hi;
+    if constexpr (kE5) {
+        lo = __builtin_amdgcn_cvt_pk_f32_bf8(int(w), false);
+        hi = __builtin_amdgcn_cvt_pk_f32_bf8(int(w), true);
+    } else {
+        lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), false);
+        hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), true);
+    }
+    x[0] = lo[0], x[1] = lo[1], x[2] = hi[0], x[3] = hi[1];
+}
+
+// A workgroup takes a token, whose place it looks up once; a lane 8 elements of a
+// head's row, of K and then of V.  Bound by memory: a value is one instruction (4 bits)
+// or two from its code.
+template <bool kBf16, int kCache>
+__global__ void __launch_bounds__(kWg) kvx_fetch_kernel(const FetchArgs a)
+{
+    const int t = int(blockIdx.x);
+    const int r = request_at(a.b.starts, a.c.num_requests, t);
+    if (r < 0 || r >= a.c.num_requests) return;
+    const Request rq = request_of(a.c, a.b, r);
+    const int j = rq.ctx + (t - rq.first);
+    const int64_t row = t - rq.first < rq.n && j < rq.total ? slot_row(a.c, r, j) : -1;
+    const int D = a.c.dim, units = a.c.hd * D / 8;
+#pragma unroll 2
+    for (int i = int(threadIdx.x); i < 2 * units; i += kWg) {
+        const bool is_v = i >= units;
+        const int u = is_v ? i - units : i;          // 8 elements, counted through the heads
+        uint4 out = make_uint4(0, 0, 0, 0);
+        if (row >= 0) {
+            const char* const src = a.c.base + (is_v ? a.c.plane_bytes : 0) + row * a.c.row_bytes;
+            if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
+                out = *reinterpret_cast<const uint4*>(src + int64_t(u) * 16);
+                if constexpr ((kCache == KVX_BF16) != kBf16) {
+                    float x[8];
+                    widen<kCache == KVX_BF16>(out, x);
+                    out = narrow<kBf16>(x);
+                }
+            } else if constexpr (kCache == KVX_FP4_E2M1) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(src + int64_t(u) * 4);
+                const uint32_t b = a.c.groups[((is_v ? a.c.plane_scales : 0) + row) * a.c.row_groups + (u >> 2)];
+                float x[8];
+                values4(w, b, x);
+                out = narrow<kBf16>(x);
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2*>(src + int64_t(u) * 8);
+                const float s = a.c.scales[(is_v ? a.c.plane_scales : 0) + row + u * 8 / D];
+                float x[8];
+                values8<kCache == KVX_FP8_E5M2>(w.x, x);
+                values8<kCache == KVX_FP8_E5M2>(w.y, x + 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] *= s;
+                    // rounded to fp32 first: a mixed-precision multiply-add would round the exact product
+                    __asm__ volatile("" : "+v"(x[e]));
+                }
+                out = narrow<kBf16>(x);
+            }
+        }
+        uint16_t* const dst = is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride;
+        *reinterpret_cast<uint4*>(dst + int64_t(u) * 8) = out;
     }
 }
 
@@ -349,7 +466,7 @@ typedef uint32_t piece_t __attribute__((ext_vector_type(4)));
 // What a lane holds of a group.
 struct Held {
     piece_t x[kHold];
-    float s[kHold];
+    float s[kHold];                              // its row's scale; 4-bit codes: its group's byte
     int64_t to[kHold];                           // row it goes to, -1: none
 };
 
@@ -387,6 +504,7 @@ __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
     const int64_t plane = int64_t(2) * layer + kv;
     char* const base = a.c.base + plane * a.c.plane_bytes;
     float* const scales = a.c.scales ? a.c.scales + plane * a.c.plane_scales : nullptr;
+    uint8_t* const groups = a.c.groups ? a.c.groups + plane * a.c.plane_scales * a.c.row_groups : nullptr;
     const int pieces = a.c.row_bytes >> 4, lg = a.lg_lanes;
     const int sets = min(kWg >> lg, kWg / kHold), group = sets * kHold;
     const int set = tid >> lg, piece = tid & ((1 << lg) - 1);
@@ -416,7 +534,9 @@ __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
             v.to[k] = mine ? s_dst[side][row] : -1;
             const piece_t* const from = reinterpret_cast<const piece_t*>(base + src * a.c.row_bytes + at);
             v.x[k] = kOnce ? __builtin_nontemporal_load(from) : *from;
-            v.s[k] = scales ? scales[src] : 0.0f;
+            v.s[k] = scales   ? scales[src]
+                     : groups ? __uint_as_float(groups[src * a.c.row_groups + min(piece, pieces - 1)])
+                              : 0.0f;
         }
     };
     auto store = [&](const Held& v) {
@@ -425,6 +545,8 @@ __global__ void __launch_bounds__(kWg) kvx_move_kernel(const MoveArgs a)
             if (v.to[k] >= 0) {
                 *reinterpret_cast<piece_t*>(base + v.to[k] * a.c.row_bytes + at) = v.x[k];
                 if (scales && piece == 0) scales[v.to[k]] = v.s[k];
+                // 16 bytes of 4-bit codes are a group
+                if (groups) groups[v.to[k] * a.c.row_groups + piece] = uint8_t(__float_as_uint(v.s[k]));
             }
     };
     Held now, next;
@@ -471,6 +593,7 @@ __global__ void __launch_bounds__(kWg) kvx_commit_kernel(const CommitArgs a)
     if (planes <= 0) return;
     char* const base = a.c.base + plane0 * a.c.plane_bytes;
     float* const scales = a.c.scales ? a.c.scales + plane0 * a.c.plane_scales : nullptr;
+    uint8_t* const groups = a.c.groups ? a.c.groups + plane0 * a.c.plane_scales * a.c.row_groups : nullptr;
     const int pieces = a.c.hd * a.c.row_bytes >> 4, lg = a.lg_lanes;
     const int per = 1 << lg, sets = kWg >> lg, set = tid >> lg, piece0 = tid & (per - 1);
     for (int i0 = 0; i0 < rows; i0 += kWg) {
@@ -498,7 +621,10 @@ __global__ void __launch_bounds__(kWg) kvx_commit_kernel(const CommitArgs a)
                     const int64_t p = min(k, planes - 1);
                     v.x[k] = *reinterpret_cast<const piece_t*>(base + p * a.c.plane_bytes +
                                                                src * a.c.row_bytes + part * 16);
-                    v.s[k] = scales ? scales[p * a.c.plane_scales + src + head] : 0.0f;
+                    v.s[k] = scales ? scales[p * a.c.plane_scales + src + head]
+                             : groups ? __uint_as_float(
+                                            groups[(p * a.c.plane_scales + src) * a.c.row_groups + part])
+                                      : 0.0f;
                 }
                 arrived(v);
                 __syncthreads();
@@ -508,6 +634,9 @@ __global__ void __launch_bounds__(kWg) kvx_commit_kernel(const CommitArgs a)
                         if (piece < pieces)
                             *reinterpret_cast<piece_t*>(base + k * a.c.plane_bytes + dst * a.c.row_bytes + piece * 16) = v.x[k];
                         if (scales && piece < a.c.hd) scales[k * a.c.plane_scales + dst + piece] = v.s[k];
+                        if (groups && piece < pieces)
+                            groups[(k * a.c.plane_scales + dst) * a.c.row_groups + piece] =
+                                uint8_t(__float_as_uint(v.s[k]));
                     }
             }
         }
@@ -535,7 +664,21 @@ int append_as(const AppendArgs& a, int cache_dtype, void* stream)
     case KVX_FP16: return append_to<kBf16, KVX_FP16>(a, stream);
     case KVX_BF16: return append_to<kBf16, KVX_BF16>(a, stream);
     case KVX_FP8_E4M3FN: return append_to<kBf16, KVX_FP8_E4M3FN>(a, stream);
+    case KVX_FP4_E2M1: return append_to<kBf16, KVX_FP4_E2M1>(a, stream);
     default: return append_to<kBf16, KVX_FP8_E5M2>(a, stream);
+    }
+}
+
+template <bool kBf16>
+int fetch_as(const FetchArgs& a, int cache_dtype, void* stream)
+{
+    const int64_t tokens = a.b.total_tokens;
+    switch (cache_dtype) {
+    case KVX_FP16: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP16>, tokens, kWg, stream, a);
+    case KVX_BF16: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_BF16>, tokens, kWg, stream, a);
+    case KVX_FP8_E4M3FN: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP8_E4M3FN>, tokens, kWg, stream, a);
+    case KVX_FP4_E2M1: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP4_E2M1>, tokens, kWg, stream, a);
+    default: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP8_E5M2>, tokens, kWg, stream, a);
     }
 }
 
@@ -562,6 +705,8 @@ int64_t commit_groups(const CacheArgs& c, int num_layers)
 
 double append_threads(int32_t tokens) { return double(tokens) * kWg; }
 
+double fetch_threads(int32_t tokens) { return double(tokens) * kWg; }
+
 double evict_threads(const CacheArgs& c, int num_layers, int max_len)
 {
     return double(num_layers) * c.num_requests * c.hd * std::max(select_threads(max_len), 2 * kWg);
@@ -573,6 +718,11 @@ int launch_append(const AppendArgs& a, int dtype, int cache_dtype, void* stream)
 {
     return dtype == KVX_BF16 ? append_as<true>(a, cache_dtype, stream)
                              : append_as<false>(a, cache_dtype, stream);
+}
+
+int launch_fetch(const FetchArgs& a, int dtype, int cache_dtype, void* stream)
+{
+    return dtype == KVX_BF16 ? fetch_as<true>(a, cache_dtype, stream) : fetch_as<false>(a, cache_dtype, stream);
 }
 
 int launch_evict(const EvictArgs& a, int num_layers, void* stream)

@@ -20,7 +20,7 @@ import ctypes
 
 import torch
 
-from . import (BF16, E4M3FN, E5M2, FP16, _addr, _check, _i32, _lib, _need, _stream, _vp)
+from . import (BF16, E2M1, E4M3FN, E5M2, FP16, _addr, _check, _i32, _lib, _need, _stream, _vp)
 
 _i64 = ctypes.c_int64
 
@@ -71,7 +71,7 @@ if _lib.kvx_ops_version() != OPS_VERSION:
 OPERATORS = tuple(sorted([*_SIGNATURES, "kvx_ops_version"]))
 
 _CACHE_TYPES = {torch.float16: FP16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3FN,
-                torch.float8_e5m2: E5M2}
+                torch.float8_e5m2: E5M2, torch.float4_e2m1fn_x2: E2M1}
 _ROW_TYPES = {torch.float16: FP16, torch.bfloat16: BF16}
 
 
@@ -83,28 +83,39 @@ def make_cache(cache, scales, block_table, dtype=None) -> kvx_cache:
     """A decode rank's cache [layers][2][num_blocks][block_size][Hd][D] with its
     scales [layers][2][num_blocks][block_size][Hd] (None for 16 bits) and the
     block table [requests][stride] of the requests at hand.  `dtype` (E4M3FN,
-    E5M2) says what codes held as uint8 are."""
+    E5M2) says what codes held as uint8 are.  A cache of 4 bits (uint8 with dtype
+    E2M1, or float4_e2m1fn_x2) is [...][Hd][D / 2], two elements a byte, its scales
+    uint8 or float8_e8m0fnu [...][Hd][D / 32]."""
     if cache.dim() != 6 or cache.shape[1] != 2:
         raise ValueError("cache must be [layers][2][num_blocks][block_size][heads][dim], not "
                          f"{list(cache.shape)}")
     kind = _CACHE_TYPES.get(cache.dtype)
     if kind is None:
-        if cache.dtype != torch.uint8 or dtype not in (E4M3FN, E5M2):
-            raise ValueError(f"a cache of {cache.dtype} needs dtype E4M3FN or E5M2 and uint8 codes")
+        if cache.dtype != torch.uint8 or dtype not in (E4M3FN, E5M2, E2M1):
+            raise ValueError(f"a cache of {cache.dtype} needs dtype E4M3FN, E5M2 or E2M1 and uint8 codes")
         kind = dtype
     elif dtype not in (None, kind):
         raise ValueError(f"dtype {dtype} does not match {cache.dtype}")
     _need(cache, max(cache.nbytes, 1) if cache.numel() else 0, "cache")
-    if (kind in (E4M3FN, E5M2)) != (scales is not None):
-        raise ValueError("scales must be given exactly for an 8-bit cache")
-    if scales is not None:
+    if (kind in (E4M3FN, E5M2, E2M1)) != (scales is not None):
+        raise ValueError("scales must be given exactly for an 8-bit or a 4-bit cache")
+    layers, _, blocks, size, heads, dim = cache.shape
+    if kind == E2M1:
+        dim *= 2
+        if dim % 32:
+            raise ValueError(f"a row of {dim} elements is no whole number of groups of 32")
+        if scales.shape != (*cache.shape[:-1], dim // 32):
+            raise ValueError(f"scales must be {[*cache.shape[:-1], dim // 32]}, not {list(scales.shape)}")
+        if scales.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+            raise ValueError(f"scales must be uint8 or float8_e8m0fnu, not {scales.dtype}")
+        _need(scales, scales.nbytes, "scales")
+    elif scales is not None:
         if scales.shape != cache.shape[:-1]:
             raise ValueError(f"scales must be {list(cache.shape[:-1])}, not {list(scales.shape)}")
         _need(scales, scales.nbytes, "scales", torch.float32)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [requests][stride]")
     _need(block_table, block_table.nbytes, "block_table", torch.int32)
-    layers, _, blocks, size, heads, dim = cache.shape
     c = kvx_cache(layers, heads, dim, kind, size, block_table.shape[0], block_table.shape[1], 0,
                   blocks, _addr(cache), _addr(scales), _addr(block_table))
     c.ref = ctypes.addressof(c)

@@ -14,7 +14,7 @@ namespace {
 // are brought to the largest and added, always in the same order.  A wave to
 // each pair, or a workgroup's four where there are many splits; a split's sum is
 // read 16 bytes a lane, as many splits at once as lanes allow.
-template <bool kBf16, int kWaves>
+template <bool kBf16, bool kMath, int kWaves>
 __global__ void __launch_bounds__(256) kvx_join_kernel(const AttendArgs a, int lg_lanes)
 {
     __shared__ __attribute__((aligned(16))) float s_acc[4][256];
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(256) kvx_join_kernel(const AttendArgs a, int l
             total == 0.0f ? make_uint2(0, 0) : make_uint2(pack2<kBf16>(acc[0] * inv, acc[1] * inv),
                                                           pack2<kBf16>(acc[2] * inv, acc[3] * inv));
     if (a.lse && lane == 0)
-        a.lse[at] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total) - kShift<kBf16>) * kLn2;
+        a.lse[at] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total) - kShift<kMath>) * kLn2;
 }
 
 // (split, token, query head) triples, in a multiple of 4
@@ -107,19 +107,22 @@ int64_t join_groups(int32_t tokens, int32_t q_heads, int waves)
     return waves == 4 ? pairs : (pairs + 3) / 4;
 }
 
-template <bool kBf16, int kWaves>
+template <bool kBf16, bool kMath>
 int join_as(const AttendArgs& a, void* stream)
 {
     int lg_lanes = 0;
     while ((4 << lg_lanes) < a.c.dim) ++lg_lanes;
-    return launch_kernel(kvx_join_kernel<kBf16, kWaves>, join_groups(a.b.total_tokens, a.q_heads, kWaves), 256, stream,
-                         a, lg_lanes);
+    const int waves = join_waves(a.splits);
+    const int64_t groups = join_groups(a.b.total_tokens, a.q_heads, waves);
+    return waves == 4 ? launch_kernel(kvx_join_kernel<kBf16, kMath, 4>, groups, 256, stream, a, lg_lanes)
+                      : launch_kernel(kvx_join_kernel<kBf16, kMath, 1>, groups, 256, stream, a, lg_lanes);
 }
 
-int join(const AttendArgs& a, bool bf, void* stream)
+// by the type of the queries and whether weights were formed as bf16's
+int join(const AttendArgs& a, bool bf, bool four, void* stream)
 {
-    if (join_waves(a.splits) == 4) return bf ? join_as<true, 4>(a, stream) : join_as<false, 4>(a, stream);
-    return bf ? join_as<true, 1>(a, stream) : join_as<false, 1>(a, stream);
+    if (bf) return join_as<true, true>(a, stream);
+    return four ? join_as<false, true>(a, stream) : join_as<false, false>(a, stream);
 }
 
 int rows(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream)
@@ -127,6 +130,7 @@ int rows(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, v
     switch (cache_dtype) {
     case KVX_FP8_E4M3FN: return launch_rows<kCodesE4m3>(a, p, dtype, stream);
     case KVX_FP8_E5M2: return launch_rows<kCodesE5m2>(a, p, dtype, stream);
+    case KVX_FP4_E2M1: return launch_rows<kCodesE2m1>(a, p, dtype, stream);
     default: return launch_rows<kCodes16>(a, p, dtype, stream);
     }
 }
@@ -144,7 +148,7 @@ int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int c
     a.part_o = a.part_ml + 2 * plan_pairs(a, p);
     const int err = p.few ? launch_few(a, p, dtype, cache_dtype, stream)
                           : rows(a, p, dtype, cache_dtype, stream);
-    return err || p.splits == 1 ? err : join(a, bf, stream);
+    return err || p.splits == 1 ? err : join(a, bf, cache_dtype == KVX_FP4_E2M1, stream);
 }
 
 double attend_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads, const AttendPlan& p)
@@ -169,7 +173,7 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
     // slots: 128, 133), and where a 16-bit cache's slots fill the card in any case the other kernel
     // reads them faster (the same trees, 64 of them, bf16: 330 us, 362 with this one; at 512 pieces
     // both take 48).
-    p.few = p.rows <= 16 || (p.rows <= 32 && c.head_dim <= 128 &&
+    p.few = c.dtype == KVX_FP4_E2M1 ? false : p.rows <= 16 || (p.rows <= 32 && c.head_dim <= 128 &&
                              (eight_bit || pieces < 512));
     p.tile_rows = p.few ? (p.rows <= 16 ? 16 : 32) : p.rows <= 64 ? 64 : 128;
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;

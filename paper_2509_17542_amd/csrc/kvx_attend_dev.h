@@ -16,7 +16,7 @@ namespace kvx {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
-enum Codes : int { kCodes16 = 0, kCodesE4m3 = 1, kCodesE5m2 = 2 };
+enum Codes : int { kCodes16 = 0, kCodesE4m3 = 1, kCodesE5m2 = 2, kCodesE2m1 = 3 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -84,6 +84,38 @@ __device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi)
 {
     return u32x4{widen2<kBf16, kCodes, false>(lo), widen2<kBf16, kCodes, true>(lo),
                  widen2<kBf16, kCodes, false>(hi), widen2<kBf16, kCodes, true>(hi)};
+}
+
+// Codes of 4 bits are values of bf16 exactly, their group's scale in them: over such a
+// cache products are bf16, and fp16 queries (and their weights) are taken as two bf16
+// terms, which hold their 11 bits.
+template <bool kBf16, int kCodes>
+constexpr bool kMathBf16 = kBf16 || kCodes == kCodesE2m1;
+
+// the factor of a group whose scale byte is b; NaN for the bytes that stand for none
+__device__ __forceinline__ float group_factor(uint32_t b) { return __uint_as_float((b > 252u ? 255u : b) << 23); }
+
+// byte kByte of a dword of 4-bit codes -> a pair of bf16
+template <int kByte>
+__device__ __forceinline__ uint32_t widen4(uint32_t w, float scale)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, kByte));
+}
+
+// 8 codes of 4 bits -> 8 bf16 values
+__device__ __forceinline__ u32x4 widen4x8(uint32_t w, float scale)
+{
+    return u32x4{widen4<0>(w, scale), widen4<1>(w, scale), widen4<2>(w, scale), widen4<3>(w, scale)};
+}
+
+// an fp16 pair as two pairs of bf16 that sum to it (an infinity is its first alone)
+__device__ __forceinline__ uint32_t two_terms(uint32_t h, uint32_t& rest)
+{
+    const float a = value16<false>(h & 0xFFFFu), b = value16<false>(h >> 16);
+    const uint32_t w = pack2<true>(a, b);
+    rest = pack2<true>(__builtin_fabsf(a) < INFINITY ? a - value16<true>(w & 0xFFFFu) : 0.0f,
+                       __builtin_fabsf(b) < INFINITY ? b - value16<true>(w >> 16) : 0.0f);
+    return w;
 }
 
 // Half `hi` (elements 2w, 2w + 1 of a row) of two keys -> their pair

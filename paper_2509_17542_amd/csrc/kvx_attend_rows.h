@@ -55,7 +55,8 @@ template <int kCodes, int DP, int NW>
 struct Shape {
     static constexpr int kWg = 64 * NW;
     static constexpr int KT = DP >= 256 || NW == 2 ? 32 : 64; // slots of a tile
-    static constexpr int kEl = kCodes == kCodes16 ? 2 : 1;
+    static constexpr int kEl = kCodes == kCodes16 ? 2 : 1;  // bytes an element (4-bit codes: kKPiece, kVPiece)
+    static constexpr int kKPiece = kCodes == kCodesE2m1 ? 4 : 8 * kEl, kVPiece = kKPiece / 2;
     static constexpr int kKRow = DP * 2 + 16;               // LDS bytes of a slot's K
     // LDS bytes of an element's V: KT / 8 pieces of 8 slots, piece g at place g ^ (d / 16 % 4),
     // so that neither the writes (a lane to every 4 elements) nor the reads meet in a bank
@@ -73,9 +74,10 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 {
     using S = Shape<kCodes, DP, NW>;
     constexpr int KT = S::KT, kWg = S::kWg, ST = KT / 32, DTB = DP / 32;
-    constexpr bool k8 = kCodes != kCodes16;
+    constexpr bool k8 = kCodes == kCodesE4m3 || kCodes == kCodesE5m2;
+    constexpr bool k4 = kCodes == kCodesE2m1, kMath = kMathBf16<kBf16, kCodes>, kTwo = k4 && !kBf16;
     constexpr bool kLift = k8 && !kBf16;
-    constexpr float kUp = kLift ? kShift<kBf16> - kLiftShift : kShift<kBf16>;
+    constexpr float kUp = kLift ? kShift<kMath> - kLiftShift : kShift<kMath>;
     constexpr uint64_t kAll = KT == 64 ? ~uint64_t(0) : (uint64_t(1) << (KT & 63)) - 1;
     __shared__ __attribute__((aligned(16))) char s_k[2][KT * S::kKRow];
     __shared__ __attribute__((aligned(16))) char s_v[2][DP * S::kVRow];
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     const int64_t token = rq.first + tok;
     const int qpos = a.b.positions ? a.b.positions[token] : rq.ctx + tok;
     const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
-    u32x4 q[DP / 16];
+    u32x4 q[DP / 16], q_rest[kTwo ? DP / 16 : 1];
     {
         const uint16_t* const src = a.q + token * a.q_stride + int64_t(head) * D;
 #pragma unroll
@@ -127,6 +129,13 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             const int d = c * 16 + half * 8;
             q[c] = u32x4{0, 0, 0, 0};
             if (live && d < D) q[c] = *reinterpret_cast<const u32x4*>(src + d);
+            if constexpr (kTwo)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t more;
+                    q[c][w] = two_terms(q[c][w], more);
+                    q_rest[c][w] = more;
+                }
         }
     }
     const ScoreArgs sc = score_args(a);
@@ -180,9 +189,13 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     // row's end its first piece: what comes of the former is masked (store, use),
     // of the latter multiplied by q's zeros or not written.
     static_assert(S::kKUnits % kWg == 0 && kWg % (DP / 4) == 0, "a thread's pieces lie at one place of the rows");
-    const int k_piece = tid % (DP / 8) * 8 * S::kEl, v_piece = tid % (DP / 4) * 4 * S::kEl;
+    const int k_piece = tid % (DP / 8) * S::kKPiece, v_piece = tid % (DP / 4) * S::kVPiece;
     const char* const k_base = kb + (k_piece < a.c.row_bytes ? k_piece : 0);
     const char* const v_base = vb + (v_piece < a.c.row_bytes ? v_piece : 0);
+    // 4-bit codes: a piece's group is numbered like its 16 bytes of codes; its scale byte goes with it
+    const int k_place = k_piece < a.c.row_bytes ? k_piece : 0, v_place = v_piece < a.c.row_bytes ? v_piece : 0;
+    const uint8_t* const kg = a.c.groups;
+    const uint8_t* const vg = a.c.groups + a.c.plane_scales * a.c.row_groups;
     u32x4 kr[S::kKPer];
     uint2 vr[S::kVPer][8];
     int64_t k_off[S::kKPer], v_off[S::kVPer][8];
@@ -206,7 +219,10 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
         for (int i = 0; i < S::kKPer; ++i) {
             const char* const p = k_base + k_off[i];
-            if constexpr (k8) {
+            if constexpr (k4) {
+                kr[i].x = *reinterpret_cast<const uint32_t*>(p);
+                kr[i].y = kg[(k_off[i] + k_place) >> 4];
+            } else if constexpr (k8) {
                 const uint2 w = *reinterpret_cast<const uint2*>(p);
                 kr[i].x = w.x, kr[i].y = w.y;
             } else {
@@ -218,7 +234,9 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const char* const p = v_base + v_off[i][e];
-                if constexpr (k8)
+                if constexpr (k4)
+                    vr[i][e] = make_uint2(*reinterpret_cast<const uint16_t*>(p), vg[(v_off[i][e] + v_place) >> 4]);
+                else if constexpr (k8)
                     vr[i][e].x = *reinterpret_cast<const uint32_t*>(p);
                 else
                     vr[i][e] = *reinterpret_cast<const uint2*>(p);
@@ -256,6 +274,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             const int key = unit / (DP / 8), d = unit % (DP / 8) * 8;
             u32x4 w = kr[i];
             if constexpr (k8) w = widen8<kBf16, kCodes>(kr[i].x, kr[i].y);
+            if constexpr (k4) w = widen4x8(kr[i].x, group_factor(kr[i].y));
             *reinterpret_cast<u32x4*>(ks + key * S::kKRow + d * 2) = w;
         }
 #pragma unroll
@@ -264,6 +283,13 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             if (S::kVUnits % kWg && unit >= S::kVUnits) break;
             const int kg = unit / (DP / 4), d = unit % (DP / 4) * 4;
             char* const out = vs + d * S::kVRow + (kg ^ ((d >> 4) & 3)) * 16;
+            if constexpr (k4) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float by = group_factor(vr[i][e].y);
+                    vr[i][e] = make_uint2(widen4<0>(vr[i][e].x, by), widen4<1>(vr[i][e].x, by));
+                }
+            }
             if (whole) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4*>(out + e * S::kVRow) = column(vr[i], e);
@@ -274,14 +300,14 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     x[e] = valid >> (first + (e & 3) + (e >> 2) * 8) & 1 ? vr[i][e] : make_uint2(0, 0);
-                    found |= nonfinite<kBf16, kCodes>(x[e].x);
-                    if constexpr (!k8) found |= nonfinite<kBf16, kCodes>(x[e].y);
+                    found |= nonfinite<kMath, k8 ? kCodes : kCodes16>(x[e].x);
+                    if constexpr (!k8) found |= nonfinite<kMath, kCodes16>(x[e].y);
                 }
                 if (found) s_special = 1;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const u32x4 w = column(x, e);
-                    *reinterpret_cast<u32x4*>(out + e * S::kVRow) = found ? classify8<kBf16>(w, 0) : w;
+                    *reinterpret_cast<u32x4*>(out + e * S::kVRow) = found ? classify8<kMath>(w, 0) : w;
                     __builtin_amdgcn_sched_barrier(0);  // one at a time: this path is rare
                 }
             }
@@ -306,8 +332,11 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
-            for (int e = 0; e < ST; ++e)
-                s[e] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(kl + e * 32 * S::kKRow + c * 32), q[c], s[e]);
+            for (int e = 0; e < ST; ++e) {
+                const u32x4 f = *reinterpret_cast<const u32x4*>(kl + e * 32 * S::kKRow + c * 32);
+                s[e] = mfma32<kMath>(f, q[c], s[e]);
+                if constexpr (kTwo) s[e] = mfma32<kMath>(f, q_rest[c], s[e]);
+            }
         // Scores relative to the row's reference so far; element i of s[e] is slot
         // 32 e + 8 (i / 4) + 4 half + i % 4.
         float base = (m == -INFINITY ? 0.0f : m) - kUp;
@@ -459,7 +488,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             }
             by_lift = __builtin_amdgcn_exp2f(lift);
         }
-        u32x4 pf[ST][2];
+        u32x4 pf[ST][2], rest[kTwo ? ST : 1][2];
 #pragma unroll
         for (int e = 0; e < ST; ++e)
 #pragma unroll
@@ -471,17 +500,26 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 } else {
                     weights(e, b, p);
                 }
-                pf[e][b >> 1][2 * (b & 1)] = pack2<kBf16>(p[0], p[1]);
-                pf[e][b >> 1][2 * (b & 1) + 1] = pack2<kBf16>(p[2], p[3]);
+                const int w = 2 * (b & 1);
+                u32x4& f = pf[e][b >> 1];
+                f[w] = pack2<kMath>(p[0], p[1]);
+                f[w + 1] = pack2<kMath>(p[2], p[3]);
+                if constexpr (kTwo) {
+                    u32x4& g = rest[e][b >> 1];
+                    g[w] = pack2<true>(p[0] - value16<true>(f[w] & 0xFFFFu), p[1] - value16<true>(f[w] >> 16));
+                    g[w + 1] = pack2<true>(p[2] - value16<true>(f[w + 1] & 0xFFFFu), p[3] - value16<true>(f[w + 1] >> 16));
+                }
             }
 #pragma unroll
         for (int e = 0; e < ST; ++e)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int t2 = 0; t2 < DTB; ++t2)
-                    o[t2] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + (b ^ (t2 & 1)) * 32),
-                                          pf[e][b], o[t2]);
+                for (int t2 = 0; t2 < DTB; ++t2) {
+                    const u32x4 f = *reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + (b ^ (t2 & 1)) * 32);
+                    o[t2] = mfma32<kMath>(f, pf[e][b], o[t2]);
+                    if constexpr (kTwo) o[t2] = mfma32<kMath>(f, rest[e][b], o[t2]);
+                }
     };
 
     if (tiles > 0) {
@@ -530,7 +568,8 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 const int first = (t & (S::kRing - 1)) * KT;
 #pragma unroll 1
                 for (int t2 = 0; t2 < DTB; ++t2) {
-                    const int byte = (32 * t2 + n32) * S::kEl, at = byte < a.c.row_bytes ? byte : 0;
+                    const int el = 32 * t2 + n32, byte = k4 ? el >> 1 : el * S::kEl;
+                    const int at = byte < a.c.row_bytes ? byte : 0;
 #pragma unroll 1
                     for (int e = 0; e < 2 * ST; ++e) {
                         u32x4 f = {0, 0, 0, 0}, seen;
@@ -538,20 +577,23 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
 #pragma unroll
                         for (int w = 0; w < 4; ++w) {
                             const uint32_t two = uint32_t(mine >> (16 * e + 8 * (w >> 1) + 2 * (w & 1))) & 3u;
-                            seen[w] = (two & 1u ? kOne<kBf16> : 0u) | (two & 2u ? kOne<kBf16> << 16 : 0u);
+                            seen[w] = (two & 1u ? kOne<kMath> : 0u) | (two & 2u ? kOne<kMath> << 16 : 0u);
 #pragma unroll
                             for (int s = 0; s < 2; ++s) {
                                 const int slot = 16 * e + 8 * (w >> 1) + 4 * half + 2 * (w & 1) + s;
                                 const char* const from = vb + s_off[first + slot] + at;
                                 uint32_t x;
-                                if constexpr (k8)
+                                if constexpr (k4)
+                                    x = widen4<0>(uint32_t(*reinterpret_cast<const uint8_t*>(from)) >> (4 * (el & 1)),
+                                                  group_factor(vg[(s_off[first + slot] + at) >> 4])) & 0xFFFFu;
+                                else if constexpr (k8)
                                     x = times2<kBf16>(widen2<kBf16, kCodes, false>(*reinterpret_cast<const uint8_t*>(from)),
                                                       scale_kind(s_vs[first + slot]), 0.0f) & 0xFFFFu;
                                 else
                                     x = *reinterpret_cast<const uint16_t*>(from);
                                 f[w] |= (valid >> slot & 1 ? x : 0u) << (16 * s);
                             }
-                            some |= nonfinite<kBf16, kCodes16>(f[w]);
+                            some |= nonfinite<kMath, kCodes16>(f[w]);
                         }
                         if (!__any(some != 0)) continue;
 #pragma unroll
@@ -559,7 +601,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                             f32x16 count;
 #pragma unroll
                             for (int i = 0; i < 16; ++i) count[i] = 0.0f;
-                            count = mfma32<kBf16>(classify8<kBf16>(f, kind), seen, count);
+                            count = mfma32<kMath>(classify8<kMath>(f, kind), seen, count);
 #pragma unroll
                             for (int i = 0; i < 16; ++i) had.add(16 * t2 + i, count[i], kind);
                         }
@@ -614,7 +656,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                     if (d < D) *reinterpret_cast<uint2*>(out + d) = w;
                 }
             if (a.lse && half == 0)
-                a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kShift<kBf16>) * kLn2;
+                a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kShift<kMath>) * kLn2;
         }
     }
 }

@@ -314,7 +314,6 @@ extern "C" kvx_status kvx_attend(const kvx_cache* c, const kvx_batch* b, const k
     KVX_TRY(check_scores(c, b, s, layer, dtype, q_heads, &idle));
     if (idle) return KVX_OK;
     KVX_TRY(check_buffers(*c));
-    if (is_fp4(c->dtype)) return fail(KVX_EUNSUPPORTED, "kvx_attend over a 4-bit cache");
     KVX_TRY(check_rows("q", q, q_stride, int64_t(q_heads) * c->head_dim));
     KVX_TRY(check_rows("out", out, out_stride, int64_t(q_heads) * c->head_dim));
     const uint64_t need = kvx::attend_workspace(*c, *b, q_heads);

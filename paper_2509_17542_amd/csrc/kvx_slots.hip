@@ -250,7 +250,6 @@ __global__ void __launch_bounds__(kWg) kvx_fetch_kernel(const FetchArgs a)
     const int j = rq.ctx + (t - rq.first);
     const int64_t row = t - rq.first < rq.n && j < rq.total ? slot_row(a.c, r, j) : -1;
     const int D = a.c.dim, units = a.c.hd * D / 8;
-#pragma unroll 2
     for (int i = int(threadIdx.x); i < 2 * units; i += kWg) {
         const bool is_v = i >= units;
         const int u = is_v ? i - units : i;          // 8 elements, counted through the heads

@@ -75,7 +75,7 @@ typedef struct {
     int64_t num_blocks;         /* pages per (layer, k/v) plane */
     void *cache;                /* device, 16-byte aligned */
     float *scales;              /* device, non-NULL if and only if dtype is 8-bit or 4-bit (the
-                                 * scale bytes then, cast) */
+                                 * scale bytes then, cast, 16-byte aligned) */
     const int32_t *block_table; /* device [num_requests][bt_stride] */
 } kvx_cache;
 

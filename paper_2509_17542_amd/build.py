@@ -27,8 +27,8 @@ SOURCES = [("kvx_kernels.hip", True), ("kvx_plan.cpp", False), ("kvx_pipe.cpp", 
            ("kvx_attend.hip", True), ("kvx_attend_few.hip", True),
            ("kvx_attend_rows_16.hip", True), ("kvx_attend_rows_e4m3.hip", True),
            ("kvx_attend_rows_e5m2.hip", True),
-           ("kvx_attend_rows_e2m1.hip", True), ("kvx_weigh.hip", True), ("kvx_verify.cpp", False),
-           ("kvx_verify.hip", True)]
+           ("kvx_attend_rows_e2m1.hip", True), ("kvx_attend_fp4.hip", True), ("kvx_weigh.hip", True),
+           ("kvx_verify.cpp", False), ("kvx_verify.hip", True)]
 
 
 def build(verbose: bool = False) -> str:

@@ -146,6 +146,11 @@ int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int c
     a.splits = p.splits;
     a.part_ml = static_cast<float*>(workspace);
     a.part_o = a.part_ml + 2 * plan_pairs(a, p);
+    if (p.few && cache_dtype == KVX_FP4_E2M1) {
+        a.ranges = p.ranges;
+        a.part_ml = static_cast<float*>(workspace);
+        return launch_few_fp4(a, p, dtype, stream);
+    }
     const int err = p.few ? launch_few(a, p, dtype, cache_dtype, stream)
                           : rows(a, p, dtype, cache_dtype, stream);
     return err || p.splits == 1 ? err : join(a, bf, cache_dtype == KVX_FP4_E2M1, stream);
@@ -153,6 +158,7 @@ int launch_attend(const AttendArgs& given, const AttendPlan& p, int dtype, int c
 
 double attend_threads(const kvx_cache& c, const kvx_batch& b, int32_t q_heads, const AttendPlan& p)
 {
+    if (p.few && c.dtype == KVX_FP4_E2M1) return threads_fp4(c, b, q_heads, p);
     // the rows kernel has a wave to 32 rows
     const int threads = p.few ? 256 : 2 * p.tile_rows;
     const double first = double(c.num_requests) * c.num_kv_heads * p.splits * p.row_tiles * threads;
@@ -173,7 +179,14 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
     // slots: 128, 133), and where a 16-bit cache's slots fill the card in any case the other kernel
     // reads them faster (the same trees, 64 of them, bf16: 330 us, 362 with this one; at 512 pieces
     // both take 48).
-    p.few = c.dtype == KVX_FP4_E2M1 ? false : p.rows <= 16 || (p.rows <= 32 && c.head_dim <= 128 &&
+    // that kernel numbers a plane's groups with 32 bits
+    if (c.dtype == KVX_FP4_E2M1 && p.rows <= 16 &&
+        double(c.num_blocks) * c.block_size * c.num_kv_heads * (c.head_dim / 32) < 0x1p32) {
+        p.few = true;
+        plan_few_fp4(c, b, p);
+        return p;
+    }
+    p.few = p.rows <= 16 || (p.rows <= 32 && c.head_dim <= 128 && c.dtype != KVX_FP4_E2M1 &&
                              (eight_bit || pieces < 512));
     p.tile_rows = p.few ? (p.rows <= 16 ? 16 : 32) : p.rows <= 64 ? 64 : 128;
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
@@ -201,6 +214,7 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
 uint64_t attend_workspace(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
 {
     const AttendPlan p = attend_plan(c, b, q_heads);
+    if (p.few && c.dtype == KVX_FP4_E2M1) return workspace_fp4(c, p);
     if (p.splits == 1) return 0;
     const uint64_t pairs = (uint64_t(b.total_tokens) * q_heads * p.splits + 3) & ~uint64_t(3);
     return pairs * (2 + uint64_t(c.head_dim)) * 4;

@@ -55,6 +55,8 @@ kvx_status check_buffers(const kvx_cache& c)
     if (!aligned16(c.cache)) return fail(KVX_EINVAL, "the cache must be 16-byte aligned");
     if ((is_fp8(c.dtype) || is_fp4(c.dtype)) != (c.scales != nullptr))
         return fail(KVX_EINVAL, "scales must be given exactly for an 8-bit or a 4-bit cache");
+    if (is_fp4(c.dtype) && !aligned16(c.scales))
+        return fail(KVX_EINVAL, "the scale bytes must be 16-byte aligned");
     return KVX_OK;
 }
 

@@ -125,6 +125,7 @@ struct AttendArgs {
     // leave their sums here for kvx_join_kernel: part_o [split][N][q_heads][dim] and
     // part_ml [split][N][q_heads] pairs (reference, sum of weights)
     int32_t chunk, splits;
+    int32_t ranges;              // kvx_attend_fp4_kernel: ranges of turns, 0: one for each request
     float* part_o;
     float* part_ml;
 };
@@ -132,13 +133,20 @@ struct AttendArgs {
 // How a call is cut into workgroups.
 struct AttendPlan {
     int rows;            // query rows of a KV head, at most
-    bool few;            // kvx_attend_few_kernel, else kvx_attend_rows_kernel
+    bool few;            // kvx_attend_few_kernel (4-bit codes: kvx_attend_fp4_kernel), else
+                         // kvx_attend_rows_kernel
     int row_tiles;       // workgroups along the rows (1 for few)
     int tile_rows;       // rows of a workgroup
     int chunk, splits;
+    int heads, ranges;   // kvx_attend_fp4_kernel: KV heads that a workgroup takes together, ranges of turns
 };
 AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads);
 int launch_few(const AttendArgs& a, const AttendPlan& p, int dtype, int cache_dtype, void* stream);
+int launch_few_fp4(const AttendArgs& a, const AttendPlan& p, int dtype, void* stream);
+// Its part of the plan, the workspace and the threads of its largest launch.
+void plan_few_fp4(const kvx_cache& c, const kvx_batch& b, AttendPlan& p);
+uint64_t workspace_fp4(const kvx_cache& c, const AttendPlan& p);
+double threads_fp4(const kvx_cache& c, const kvx_batch& b, int32_t q_heads, const AttendPlan& p);
 template <int kCodes>
 int launch_rows(const AttendArgs& a, const AttendPlan& p, int dtype, void* stream);
 

@@ -53,6 +53,7 @@ def test_four_bit_caches_are_refused():
             assert call(c=four(head_dim=dim)) == K.EINVAL
         assert call(c=four(head_dim=288)) == K.EUNSUPPORTED
         assert call(c=four(scales=None)) == K.EINVAL
+        assert call(c=four(scales=GOOD + 4)) == K.EINVAL
         assert call(c=four(cache=None)) == K.EINVAL
 
 

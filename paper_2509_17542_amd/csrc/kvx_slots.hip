@@ -237,44 +237,83 @@ __device__ __forceinline__ void values8(uint32_t w, float* x)
     x[0] = lo[0], x[1] = lo[1], x[2] = hi[0], x[3] = hi[1];
 }
 
-// A workgroup takes a token, whose place it looks up once; a lane 8 elements of a
-// head's row, of K and then of V.  Bound by memory: a value is one instruction (4 bits)
-// or two from its code.
+constexpr int kFetchTokens = 16;
+
+// A workgroup takes `tokens` of them (16 where there are enough to fill the card), whose places
+// are looked up side by side first; a lane takes 8 elements of a head's row, of K and then of V, four
+// at a time.  Bound by memory: a value is one instruction (4 bits) or two from its code.
+// Requests of 1000..6000 slots out of a 4-bit cache (334 MB) took 111 us with a token a
+// workgroup, most of it the chain of lookups.
 template <bool kBf16, int kCache>
-__global__ void __launch_bounds__(kWg) kvx_fetch_kernel(const FetchArgs a)
+__global__ void __launch_bounds__(kWg) kvx_fetch_kernel(const FetchArgs a, int tokens, FastDiv div_units, FastDiv div_row)
 {
-    const int t = int(blockIdx.x);
-    const int r = request_at(a.b.starts, a.c.num_requests, t);
-    if (r < 0 || r >= a.c.num_requests) return;
-    const Request rq = request_of(a.c, a.b, r);
-    const int j = rq.ctx + (t - rq.first);
-    const int64_t row = t - rq.first < rq.n && j < rq.total ? slot_row(a.c, r, j) : -1;
-    const int D = a.c.dim, units = a.c.hd * D / 8;
-    for (int i = int(threadIdx.x); i < 2 * units; i += kWg) {
-        const bool is_v = i >= units;
-        const int u = is_v ? i - units : i;          // 8 elements, counted through the heads
-        uint4 out = make_uint4(0, 0, 0, 0);
-        if (row >= 0) {
-            const char* const src = a.c.base + (is_v ? a.c.plane_bytes : 0) + row * a.c.row_bytes;
+    __shared__ int64_t s_row[kFetchTokens];      // -1: zeros, -2: not written
+    const int t0 = int(blockIdx.x) * tokens, end = min(tokens, a.b.total_tokens - t0);
+    if (threadIdx.x < 64) {
+        const int first = request_at(a.b.starts, a.c.num_requests, t0);
+        if (int(threadIdx.x) < end) {
+            const int t = t0 + int(threadIdx.x);
+            int r = first;
+            while (r >= -1 && r < a.c.num_requests && a.b.starts[r + 1] <= t) ++r;
+            int64_t row = -2;
+            if (r >= 0 && r < a.c.num_requests) {
+                const Request rq = request_of(a.c, a.b, r);
+                const int j = rq.ctx + (t - rq.first);
+                row = t - rq.first < rq.n && j < rq.total ? slot_row(a.c, r, j) : -1;
+            }
+            s_row[threadIdx.x] = row;
+        }
+    }
+    __syncthreads();
+    // units: 8 elements, counted through a token's heads, K's and then V's, and through the tokens
+    const int units = int(a.c.hd) * a.c.dim / 8;
+    const uint32_t all = uint32_t(end) * 2u * uint32_t(units);
+    constexpr int kAtOnce = 4;
+    for (uint32_t i0 = threadIdx.x; i0 < all; i0 += kAtOnce * kWg) {
+        uint4 w[kAtOnce];
+        uint32_t extra[kAtOnce];
+        int64_t row[kAtOnce];
+        uint16_t* dst[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const uint32_t i = min(i0 + k * kWg, all - 1), side = fast_div(i, div_units);   // 2 x token + (0: K, 1: V)
+            const int u = int(i - side * uint32_t(units));
+            const int t = int(side >> 1);
+            const bool is_v = side & 1;
+            row[k] = i0 + k * kWg < all ? s_row[t] : -2;
+            dst[k] = (is_v ? a.v + (t0 + t) * a.v_stride : a.k + (t0 + t) * a.k_stride) + int64_t(u) * 8;
+            const int64_t at = max(row[k], int64_t(0));
+            const char* const src = a.c.base + (is_v ? a.c.plane_bytes : 0) + at * a.c.row_bytes;
             if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
-                out = *reinterpret_cast<const uint4*>(src + int64_t(u) * 16);
+                w[k] = *reinterpret_cast<const uint4*>(src + int64_t(u) * 16);
+            } else if constexpr (kCache == KVX_FP4_E2M1) {
+                w[k].x = *reinterpret_cast<const uint32_t*>(src + int64_t(u) * 4);
+                extra[k] = a.c.groups[((is_v ? a.c.plane_scales : 0) + at) * a.c.row_groups + (u >> 2)];
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(src + int64_t(u) * 8);
+                w[k].x = x.x, w[k].y = x.y;
+                extra[k] = __float_as_uint(a.c.scales[(is_v ? a.c.plane_scales : 0) + at + fast_div(uint32_t(u), div_row)]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            if (row[k] < -1) continue;
+            uint4 out = w[k];
+            if constexpr (kCache == KVX_FP16 || kCache == KVX_BF16) {
                 if constexpr ((kCache == KVX_BF16) != kBf16) {
                     float x[8];
                     widen<kCache == KVX_BF16>(out, x);
                     out = narrow<kBf16>(x);
                 }
             } else if constexpr (kCache == KVX_FP4_E2M1) {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(src + int64_t(u) * 4);
-                const uint32_t b = a.c.groups[((is_v ? a.c.plane_scales : 0) + row) * a.c.row_groups + (u >> 2)];
                 float x[8];
-                values4(w, b, x);
+                values4(w[k].x, extra[k], x);
                 out = narrow<kBf16>(x);
             } else {
-                const uint2 w = *reinterpret_cast<const uint2*>(src + int64_t(u) * 8);
-                const float s = a.c.scales[(is_v ? a.c.plane_scales : 0) + row + u * 8 / D];
+                const float s = __uint_as_float(extra[k]);
                 float x[8];
-                values8<kCache == KVX_FP8_E5M2>(w.x, x);
-                values8<kCache == KVX_FP8_E5M2>(w.y, x + 4);
+                values8<kCache == KVX_FP8_E5M2>(w[k].x, x);
+                values8<kCache == KVX_FP8_E5M2>(w[k].y, x + 4);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     x[e] *= s;
@@ -283,9 +322,9 @@ __global__ void __launch_bounds__(kWg) kvx_fetch_kernel(const FetchArgs a)
                 }
                 out = narrow<kBf16>(x);
             }
+            if (row[k] < 0) out = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(dst[k]) = out;
         }
-        uint16_t* const dst = is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride;
-        *reinterpret_cast<uint4*>(dst + int64_t(u) * 8) = out;
     }
 }
 
@@ -668,16 +707,32 @@ int append_as(const AppendArgs& a, int cache_dtype, void* stream)
     }
 }
 
+// tokens of a workgroup: as many as leave each CU eight of those
+int fetch_tokens(int32_t tokens) { return std::min(kFetchTokens, std::max(1, tokens / 2048)); }
+
+int64_t fetch_groups(int32_t tokens)
+{
+    const int each = fetch_tokens(tokens);
+    return (int64_t(tokens) + each - 1) / each;
+}
+
+template <bool kBf16, int kCache>
+int fetch_by(const FetchArgs& a, void* stream)
+{
+    return launch_kernel(kvx_fetch_kernel<kBf16, kCache>, fetch_groups(a.b.total_tokens), kWg, stream, a,
+                         fetch_tokens(a.b.total_tokens), make_fastdiv(uint32_t(a.c.hd) * a.c.dim / 8),
+                         make_fastdiv(uint32_t(a.c.dim) / 8));
+}
+
 template <bool kBf16>
 int fetch_as(const FetchArgs& a, int cache_dtype, void* stream)
 {
-    const int64_t tokens = a.b.total_tokens;
     switch (cache_dtype) {
-    case KVX_FP16: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP16>, tokens, kWg, stream, a);
-    case KVX_BF16: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_BF16>, tokens, kWg, stream, a);
-    case KVX_FP8_E4M3FN: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP8_E4M3FN>, tokens, kWg, stream, a);
-    case KVX_FP4_E2M1: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP4_E2M1>, tokens, kWg, stream, a);
-    default: return launch_kernel(kvx_fetch_kernel<kBf16, KVX_FP8_E5M2>, tokens, kWg, stream, a);
+    case KVX_FP16: return fetch_by<kBf16, KVX_FP16>(a, stream);
+    case KVX_BF16: return fetch_by<kBf16, KVX_BF16>(a, stream);
+    case KVX_FP8_E4M3FN: return fetch_by<kBf16, KVX_FP8_E4M3FN>(a, stream);
+    case KVX_FP4_E2M1: return fetch_by<kBf16, KVX_FP4_E2M1>(a, stream);
+    default: return fetch_by<kBf16, KVX_FP8_E5M2>(a, stream);
     }
 }
 
@@ -704,7 +759,7 @@ int64_t commit_groups(const CacheArgs& c, int num_layers)
 
 double append_threads(int32_t tokens) { return double(tokens) * kWg; }
 
-double fetch_threads(int32_t tokens) { return double(tokens) * kWg; }
+double fetch_threads(int32_t tokens) { return double(fetch_groups(tokens)) * kWg; }
 
 double evict_threads(const CacheArgs& c, int num_layers, int max_len)
 {

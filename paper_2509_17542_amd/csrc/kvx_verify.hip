@@ -7,13 +7,16 @@
 //             another child may follow;
 //   walk      a workgroup per request joins its rows' parts, decides for every token
 //             whether its parent would accept it (that does not depend on the path), and
-//             follows the path from the first; without a draft it draws the next token
-//             too: the part by the parts' sums, the token by a scan over that part;
-//   residual, draw  (draft's logits given) the same for max(r - q, 0), whose parts have
-//             to be summed first.
+//             follows the path from the first;
+//   last      (many logits) the parts of the rows after which the next tokens are drawn, again;
+//   residual  (draft's logits given) the sums of max(r - q, 0) there;
+//   draw      the part by the parts' sums, the token by a scan over that part.
 // The next token is the place where a sum over up to V terms passes a given share of
 // the whole: an error of 1e-7 of it, as of fp32 exponentials, moves thousands of such
-// borders by that much, so all sums and exponentials are 64-bit.
+// borders by that much, so what it goes by is summed in 64 bits, from exponentials of 1e-13.
+// Whether a token is accepted is one comparison, which fp32 exponentials decide otherwise
+// once in 10^7: from 2^24 logits on all rows are summed from those (80 million logits: 68 us in 64
+// bits, 27 so) and the last rows in 64 bits again; fewer are in 64 bits at once, which saves two launches.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -60,32 +63,43 @@ __device__ __forceinline__ u32x4 load16(const char* p)
     return w;
 }
 
-// exp2(x / 64), x <= 0 or near it, to 1e-13: x = 64 n + j + f, |f| <= 1/2; 2^(j / 64) out of
-// a table and the series of exp(f ln 2 / 64), whose first term left out is (ln 2 / 128)^5 / 120.
-__device__ __forceinline__ double exp2_64th(const double* table, double x)
+// exp2(x / 256) to 1e-13, -2.6e5 <= x <= 256; x = 256 n + j + f, |f| <= 1/2: 2^(j / 256) out of
+// a table, the series of exp(f ln 2 / 256), whose first term left out is (ln 2 / 512)^4 / 24, and
+// n added to the exponent.  Adding 1.5 x 2^52 rounds x to an integer, which lies in the low word.
+constexpr int kTable = 256;
+constexpr double kLeast = -2.5e5;
+
+__device__ __forceinline__ double exp2_near(const double* table, double x)
 {
-    constexpr double u = 0.69314718055994530942 / 64;
-    x = fmax(x, -1e5);                   // 2^-1500: 0
-    const double n = rint(x), f = x - n;
-    const int i = int(n);
-    double y = __builtin_fma(f, u * u * u * u / 24, u * u * u / 6);
-    y = __builtin_fma(f, y, u * u / 2);
+    constexpr double u = 0.69314718055994530942 / kTable;
+    const double whole = x + 0x1.8p52, f = x - (whole - 0x1.8p52);
+    const int i = int(uint32_t(__builtin_bit_cast(uint64_t, whole)));
+    double y = __builtin_fma(f, u * u * u / 6, u * u / 2);
     y = __builtin_fma(f, y, u);
     y = __builtin_fma(f, y, 1.0);
-    return ldexp(table[i & 63] * y, i >> 6);
+    const uint64_t w = __builtin_bit_cast(uint64_t, table[i & (kTable - 1)] * y);
+    return __builtin_bit_cast(double, uint64_t(uint32_t(w >> 32) + (uint32_t(i & -kTable) << 12)) << 32 | uint32_t(w));
+}
+
+// The same for any x <= 256, 0 below 2^-976.
+__device__ __forceinline__ double exp2_256th(const double* table, double x)
+{
+    const double y = exp2_near(table, fmax(x, kLeast));
+    return x < kLeast ? 0.0 : y;
 }
 
 __device__ __forceinline__ void fill_table(double* table)
 {
-    if (threadIdx.x < 64) table[threadIdx.x] = exp2(double(threadIdx.x) / 64);
+    for (int i = int(threadIdx.x); i < kTable; i += int(blockDim.x)) table[i] = exp2(double(i) / kTable);
 }
 
-// 64 log2(e) / T; 0: greedy
+// 256 log2(e) / T, of 40 bits: its products with 16-bit logits are exact.  0: greedy
 __device__ __forceinline__ double rate_of(const VerifyArgs& a, int r)
 {
     const float t = a.temperatures ? a.temperatures[r] : 1.0f;
     if (!(t >= 0x1p-60f)) return 0.0;
-    return 92.332482616893656877 / double(fminf(t, 0x1p60f));
+    const double rate = 369.32993046757462751 / double(fminf(t, 0x1p60f));
+    return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, rate) & ~uint64_t(0x1FFF));
 }
 
 struct Drafts {
@@ -121,24 +135,33 @@ __device__ __forceinline__ const char* row_of(const VerifyArgs& a, int side, int
 
 // ---- parts ---------------------------------------------------------------------
 
-template <int kType>
-__global__ void __launch_bounds__(kWg) kvx_verify_parts_kernel(const VerifyArgs a)
+constexpr int kLeaf = 1 << 30;           // VerifyArgs::last: nothing was refused there
+
+enum Pass : int { kFine = 0, kCoarse = 1, kLast = 2 };
+
+template <int kType, int kPass>
+__global__ void __launch_bounds__(kWg, (kPass == kCoarse ? 6 : 4)) kvx_verify_parts_kernel(const VerifyArgs a)
 {
     constexpr int kV = kVec<kType>, kEach = kPart / 64 / kV;
-    __shared__ double s_table[64];
-    fill_table(s_table);
-    __syncthreads();
+    __shared__ double s_table[kPass == kCoarse ? 1 : kTable];
+    if constexpr (kPass != kCoarse) {
+        fill_table(s_table);
+        __syncthreads();
+    }
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int64_t unit = int64_t(blockIdx.x) * kWaves + wave, rows = unit / a.parts;
-    const int c = int(unit - rows * a.parts), side = rows >= a.total_tokens;
-    const int row = int(rows - (side ? a.total_tokens : 0));
-    if (row >= a.total_tokens || (side && !a.draft)) return;
-    const int r = request_at(a.starts, a.num_requests, row);
+    const int32_t of = kPass == kLast ? a.num_requests : a.total_tokens;
+    const int c = int(unit - rows * a.parts), side = rows >= of, index = int(rows - (side ? of : 0));
+    if (index >= of || (side && !a.draft)) return;
+    const int mark = kPass == kLast ? a.last[index] : 0;
+    if (mark < 0) return;
+    const int r = kPass == kLast ? index : request_at(a.starts, a.num_requests, index);
     if (r < 0 || r >= a.num_requests) return;
     const Drafts d = drafts_of(a, r);
-    const int at = row - d.first;
+    const int at = kPass == kLast ? mark & ~kLeaf : index - d.first, row = d.first + at;
     if (at >= d.n) return;
     const double rate = rate_of(a, r);
+    if (kPass == kLast && side && mark & kLeaf) return;
     if (side) {
         // a draft's row counts where it has children
         bool some = false;
@@ -154,39 +177,49 @@ __global__ void __launch_bounds__(kWg) kvx_verify_parts_kernel(const VerifyArgs 
     const char* const x = row_of(a, side, row, kSize<kType>) + int64_t(c) * kPart * kSize<kType>;
     const int n = min(kPart, a.vocab - c * kPart);
     u32x4 w[kEach];
+    if (n == kPart) {
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int v = (k * 64 + lane) * kV;
-        if (v + kV <= n) {
-            w[k] = load16(x + v * kSize<kType>);
-        } else {
-            // past the row's end: -infinity
-            constexpr uint32_t none = kType == kF32 ? 0xFF800000u : kType == kB16 ? 0xFF80FF80u : 0xFC00FC00u;
-            w[k] = u32x4{none, none, none, none};
+        for (int k = 0; k < kEach; ++k) w[k] = load16(x + (k * 64 + lane) * 16);
+    } else {
+        // The last 16 bytes of the row again where it ends, their elements that others have, and
+        // what lies past the end, -infinity.
+        constexpr uint32_t none = kType == kF32 ? 0xFF800000u : kType == kB16 ? 0xFF80u : 0xFC00u;
 #pragma unroll
-            for (int e = 0; e < kV; ++e)
-                if (v + e < n) {
-                    if constexpr (kType == kF32) {
-                        w[k][e] = reinterpret_cast<const uint32_t*>(x)[v + e];
-                    } else {
-                        const uint32_t h = reinterpret_cast<const uint16_t*>(x)[v + e];
-                        w[k][e >> 1] = e & 1 ? (w[k][e >> 1] & 0xFFFFu) | h << 16
-                                             : (w[k][e >> 1] & 0xFFFF0000u) | h;
-                    }
+        for (int k = 0; k < kEach; ++k) {
+            const int v = (k * 64 + lane) * kV, from = max(min(v, n - kV), 0);
+            if (n >= kV) {
+                w[k] = load16(x + from * kSize<kType>);
+            } else {
+                w[k] = u32x4{0, 0, 0, 0};
+                for (int e = 0; e < n; ++e) {
+                    const uint32_t h = kType == kF32 ? reinterpret_cast<const uint32_t*>(x)[e]
+                                                     : reinterpret_cast<const uint16_t*>(x)[e];
+                    const int word = kType == kF32 ? e : e >> 1;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[k][i] |= i == word ? h << (kType == kF32 ? 0 : 16 * (e & 1)) : 0u;
                 }
+            }
+            // elements [least, most) of these are this lane's
+            const int least = v - from, most = n - from;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (kType == kF32) {
+                    if (i < least || i >= most) w[k][i] = none;
+                } else {
+                    if (2 * i < least || 2 * i >= most) w[k][i] = (w[k][i] & 0xFFFF0000u) | none;
+                    if (2 * i + 1 < least || 2 * i + 1 >= most) w[k][i] = (w[k][i] & 0xFFFFu) | none << 16;
+                }
+            }
         }
     }
+    // the largest; NaN where one is NaN
     float top = -INFINITY;
-    bool bad = false;
 #pragma unroll
     for (int k = 0; k < kEach; ++k)
 #pragma unroll
-        for (int e = 0; e < kV; ++e) {
-            const float v = element<kType>(w[k], e);
-            top = fmaxf(top, v);
-            bad |= !(v < INFINITY);
-        }
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        for (int e = 0; e < kV; ++e) top = __builtin_elementwise_maximum(top, element<kType>(w[k], e));
+    for (int o = 32; o; o >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, o));
+    const bool bad = !(top < INFINITY);
     int first = INT32_MAX;
     if (rate == 0.0) {
 #pragma unroll
@@ -197,27 +230,49 @@ __global__ void __launch_bounds__(kWg) kvx_verify_parts_kernel(const VerifyArgs 
         for (int o = 32; o; o >>= 1) first = min(first, __shfl_xor(first, o));
     }
     double sum = 0.0;
-    if (top == -INFINITY) {
+    if (bad || top == -INFINITY) {
         sum = 0.0;
     } else if (rate == 0.0) {
         sum = lane == 0 ? 1.0 : 0.0;
+    } else if constexpr (kPass == kCoarse) {
+        // log2(e) / T in two terms; differences of 200 in log2 and more are 0
+        const double by = rate * (1.0 / kTable);
+        const float hi = float(by), lo = float(by - double(hi)), least = -200.0f / hi;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            float x[kV];
+#pragma unroll
+            for (int e = 0; e < kV; ++e) {
+                const float d = fmaxf(element<kType>(w[k], e) - top, least);
+                x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, hi, d * lo));
+            }
+#pragma unroll
+            for (int n = kV / 2; n; n >>= 1)
+#pragma unroll
+                for (int e = 0; e < n; ++e) x[e] += x[e + n];
+            sum += double(x[0]);
+        }
     } else {
+        // what is far below weighs 2^-976 here
+        const double back = -double(top) * rate;
 #pragma unroll
         for (int k = 0; k < kEach; ++k)
 #pragma unroll
             for (int e = 0; e < kV; ++e) {
-                const float v = element<kType>(w[k], e);
-                sum += exp2_64th(s_table, (double(v) - double(top)) * rate);
+                const double v = double(element<kType>(w[k], e));
+                const double x = kType == kF32 ? (v - double(top)) * rate : __builtin_fma(v, rate, back);
+                sum += exp2_near(s_table, fmax(x, kLeast));
             }
     }
     sum = wave_sum(sum);
-    if (__any(bad)) sum = NAN;
-    if (lane == 0) a.part[side][int64_t(row) * a.parts + c] = Part{sum, top, first};
+    if (bad) sum = NAN;
+    Part* const out = kPass == kLast ? a.last_part[side] + int64_t(r) * a.parts : a.part[side] + int64_t(row) * a.parts;
+    if (lane == 0) out[c] = Part{sum, top, first};
 }
 
 // ---- what a row is ---------------------------------------------------------------
 
-// A row's softmax: weight exp2((l - top) rate / 64) of sum `sum`; sum 0: no distribution.
+// A row's softmax: weight exp2((l - top) rate / 256) of sum `sum`; sum 0: no distribution.
 struct Whole {
     double sum;
     float top;
@@ -234,7 +289,7 @@ __device__ __forceinline__ Whole join(const Part* part, int parts, double rate, 
     int at = INT32_MAX;
     for (int c = lane; c < parts; c += lanes) {
         const Part p = part[c];
-        const double by = exp2_64th(table, p.top == -INFINITY ? -1e5 : (double(p.top) - double(top)) * rate);
+        const double by = exp2_256th(table, p.top == -INFINITY ? 2 * kLeast : (double(p.top) - double(top)) * rate);
         sum += p.sum * (p.top == -INFINITY ? 1.0 : by);
         if (p.top == top) at = min(at, p.at);
     }
@@ -249,7 +304,7 @@ __device__ __forceinline__ Whole join(const Part* part, int parts, double rate, 
 // a logit's share of its row
 __device__ __forceinline__ double share(float l, float top, double rate, double by, const double* table)
 {
-    return exp2_64th(table, (double(l) - double(top)) * rate) * by;
+    return exp2_256th(table, (double(l) - double(top)) * rate) * by;
 }
 
 // What refusing k children leaves of one element's r; q0 is its share of the draft's row.
@@ -271,6 +326,7 @@ struct Children {
     int token[kMaxDrafted];
     double by[kMaxDrafted];              // what q is multiplied by at that child
     double left[kMaxDrafted];
+    uint8_t dull[kMaxDrafted];           // a token that an earlier sibling is, or none of the vocabulary
     int count;
 };
 
@@ -296,23 +352,28 @@ __device__ __forceinline__ void list_children(const VerifyArgs& a, const Drafts&
         if (lane == 0) s.count = count;
     }
     __syncthreads();
+    for (int j = int(threadIdx.x); j < s.count; j += int(blockDim.x)) {
+        const int x = s.token[j];
+        bool dull = x < 0 || x >= a.vocab;
+        for (int i = 0; i < j && !dull; ++i) dull = s.token[i] == x;
+        s.dull[j] = dull;
+    }
+    __syncthreads();
 }
 
-// Their q factors (thread 0's work): 1, or what is left of q without the tokens before.
+// Their q factors: 1, or what is left of q without the tokens before.
 template <int kType>
 __device__ __forceinline__ void draft_factors(const VerifyArgs& a, const char* row, const Whole& q, double rate,
                                               const double* table, Children& s)
 {
+    for (int j = int(threadIdx.x); j < s.count; j += int(blockDim.x))
+        s.left[j] = a.distinct && !s.dull[j] ? share(logit<kType>(row, s.token[j]), q.top, rate, 1.0 / q.sum, table) : 0.0;
+    __syncthreads();
     if (threadIdx.x == 0) {
         double by = 1.0;
         for (int j = 0; j < s.count; ++j) {
             s.by[j] = by;
-            if (!a.distinct) continue;
-            const int x = s.token[j];
-            bool seen = x < 0 || x >= a.vocab;
-            for (int i = 0; i < j && !seen; ++i) seen = s.token[i] == x;
-            if (seen) continue;
-            const double gone = share(logit<kType>(row, x), q.top, rate, 1.0 / q.sum, table) * by;
+            const double gone = s.left[j] * by;
             if (gone < 1.0) by /= 1.0 - gone;
         }
     }
@@ -339,7 +400,7 @@ __device__ __forceinline__ double group_sum(double x, double* s_part)
 template <int kType>
 __global__ void __launch_bounds__(kWalk) kvx_verify_siblings_kernel(const VerifyArgs a)
 {
-    __shared__ double s_table[64], s_part[kWalk / 64];
+    __shared__ double s_table[kTable], s_part[kWalk / 64];
     __shared__ Children s_kids;
     const int row = int(blockIdx.x);
     const int r = request_at(a.starts, a.num_requests, row);
@@ -353,14 +414,35 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_siblings_kernel(const Verify
     const int count = s_kids.count;
     if (count < 2) return;
     const int lane = int(threadIdx.x) & 63;
-    const Whole p = join(a.part[0] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
-    const Whole q = join(a.part[1] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
+    Whole p = join(a.part[0] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
+    Whole q = join(a.part[1] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
     if (p.sum == 0.0 || q.sum == 0.0) return;
     const char* const pr = row_of(a, 0, row, kSize<kType>);
     const char* const qr = row_of(a, 1, row, kSize<kType>);
+    constexpr int kV = kVec<kType>;
+    // over both rows: each(l, l', v) for every token
+    auto walk = [&](auto each) {
+        for (int v = int(threadIdx.x) * kV; v < a.vocab; v += kWalk * kV) {
+            if (v + kV <= a.vocab) {
+                const u32x4 x = load16(pr + int64_t(v) * kSize<kType>), y = load16(qr + int64_t(v) * kSize<kType>);
+#pragma unroll
+                for (int e = 0; e < kV; ++e) each(element<kType>(x, e), element<kType>(y, e), v + e);
+            } else {
+                for (int e = v; e < a.vocab; ++e) each(logit<kType>(pr, e), logit<kType>(qr, e), e);
+            }
+        }
+    };
+    if (a.last_part[0]) {                // the parts' sums are of fp32 exponentials
+        double sp = 0.0, sq = 0.0;
+        walk([&](float lp, float lq, int) {
+            sp += share(lp, p.top, rate, 1.0, s_table);
+            sq += share(lq, q.top, rate, 1.0, s_table);
+        });
+        p.sum = group_sum<kWalk>(sp, s_part);
+        q.sum = group_sum<kWalk>(sq, s_part);
+    }
     draft_factors<kType>(a, qr, q, rate, s_table, s_kids);
     const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;
-    constexpr int kV = kVec<kType>;
     for (int k = 0; k + 1 < count; ++k) {
         if (threadIdx.x == 0) s_kids.left[k] = 1.0;
         __syncthreads();
@@ -370,15 +452,7 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_siblings_kernel(const Verify
                            [&](int j) { return s_kids.left[j]; });
         };
         double sum = 0.0;
-        for (int v = int(threadIdx.x) * kV; v < a.vocab; v += kWalk * kV) {
-            if (v + kV <= a.vocab) {
-                const u32x4 x = load16(pr + int64_t(v) * kSize<kType>), y = load16(qr + int64_t(v) * kSize<kType>);
-#pragma unroll
-                for (int e = 0; e < kV; ++e) sum += one(element<kType>(x, e), element<kType>(y, e), v + e);
-            } else {
-                for (int e = v; e < a.vocab; ++e) sum += one(logit<kType>(pr, e), logit<kType>(qr, e), e);
-            }
-        }
+        walk([&](float lp, float lq, int v) { sum += one(lp, lq, v); });
         sum = group_sum<kWalk>(sum, s_part);
         if (threadIdx.x == 0) {
             const double left = sum > 0.0 ? 1.0 / sum : 1.0;
@@ -418,10 +492,11 @@ __device__ __forceinline__ int draw(const VerifyArgs& a, float sample, double* s
         return before + (lane ? prev : 0.0);
     };
     const float cut = sample > 0.0f ? fminf(sample, 0x1.fffffep-1f) : 0.0f;
-    // the part: consecutive ones to a thread
+    // the part: consecutive ones to a thread, the first of them kept
     const int per = (a.parts + kWalk - 1) / kWalk, c0 = min(tid * per, a.parts), c1 = min(c0 + per, a.parts);
-    double mine = 0.0, whole;
-    for (int c = c0; c < c1; ++c) mine += of_part(c);
+    const double own = c0 < c1 ? of_part(c0) : 0.0;
+    double mine = own, whole;
+    for (int c = c0 + 1; c < c1; ++c) mine += of_part(c);
     double before = scan(mine, whole);
     if (!(whole > 0.0)) return -1;
     double target = double(cut) * whole;
@@ -431,7 +506,7 @@ __device__ __forceinline__ int draw(const VerifyArgs& a, float sample, double* s
     int found = INT32_MAX, some = -1;
     double at = before;
     for (int c = c0; c < c1; ++c) {
-        const double x = of_part(c);
+        const double x = c == c0 ? own : of_part(c);
         if (x > 0.0) some = c;
         at += x;
         if (x > 0.0 && at > target && found == INT32_MAX) found = c;
@@ -443,7 +518,7 @@ __device__ __forceinline__ int draw(const VerifyArgs& a, float sample, double* s
     __syncthreads();
     if (part >= c0 && part < c1) {
         double sum = before;
-        for (int c = c0; c < part; ++c) sum += of_part(c);
+        for (int c = c0; c < part; ++c) sum += c == c0 ? own : of_part(c);
         s_scan[kWalk / 64] = sum;
     }
     if (tid == 0) s_pick[0] = INT32_MAX, s_pick[1] = -1;
@@ -472,12 +547,42 @@ __device__ __forceinline__ int draw(const VerifyArgs& a, float sample, double* s
     return s_pick[0] != INT32_MAX ? s_pick[0] : s_pick[1];
 }
 
+// Without a draft: from p with the tokens of `refusal` at 0, or all of p where that leaves nothing.
+template <int kType>
+__device__ __forceinline__ int draw_plain(const VerifyArgs& a, const char* row, const Part* part, const Whole& p,
+                                          double rate, const int* refusal, int count, float sample,
+                                          const double* table, double* s_scan, int* s_pick)
+{
+    auto weight = [&](int v) { return share(logit<kType>(row, v), p.top, rate, 1.0, table); };
+    auto of_part = [&](int c) {
+        return part[c].top == -INFINITY ? 0.0 : part[c].sum * exp2_256th(table, (double(part[c].top) - double(p.top)) * rate);
+    };
+    for (;; count = 0) {
+        const int next = draw(
+            a, sample, s_scan, s_pick,
+            [&](int c) {
+                const double all = of_part(c);
+                double x = all;
+                for (int j = 0; j < count; ++j)
+                    if (refusal[j] / kPart == c) x -= weight(refusal[j]);
+                // what rounding leaves of a part whose weight was refused
+                return x > 0x1p-40 * all ? x : 0.0;
+            },
+            [&](int v) {
+                for (int j = 0; j < count; ++j)
+                    if (refusal[j] == v) return 0.0;
+                return weight(v);
+            });
+        if (next >= 0 || count == 0) return next;
+    }
+}
+
 // ---- walk ------------------------------------------------------------------------
 
 template <int kType, bool kDraft>
 __global__ void __launch_bounds__(kWalk) kvx_verify_walk_kernel(const VerifyArgs a)
 {
-    __shared__ double s_table[64], s_scan[kWalk / 64 + 1];
+    __shared__ double s_table[kTable], s_scan[kWalk / 64 + 1];
     __shared__ Whole s_row[kDraft ? 2 : 1][kMaxDrafted];
     __shared__ int s_best[kMaxDrafted], s_parent[kMaxDrafted], s_token[kMaxDrafted], s_pick[2], s_last, s_leaf;
     __shared__ double s_own[kMaxDrafted], s_drafted[kDraft ? kMaxDrafted : 1];
@@ -584,57 +689,45 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_walk_kernel(const VerifyArgs
     if (p.sum == 0.0 || rate == 0.0) {
         if (tid == 0) {
             a.next[r] = p.sum == 0.0 ? -1 : p.at;
-            if constexpr (kDraft) a.last[r] = -1;
+            if (a.last) a.last[r] = -1;
         }
         return;
     }
-    if constexpr (kDraft) {
-        // a leaf has nothing refused: bit 30
-        if (tid == 0) a.last[r] = last | (s_leaf || s_row[1][last].sum == 0.0 ? 1 << 30 : 0);
+    if (kDraft || a.last) {
+        bool leaf = s_leaf;
+        if constexpr (kDraft) leaf |= s_row[1][last].sum == 0.0;
+        if (tid == 0) a.last[r] = last | (leaf ? kLeaf : 0);
         return;
     }
-    const char* const row = row_of(a, 0, d.first + last, kSize<kType>);
-    // the tokens refused there, each once
-    int* const refusal = s_best;
-    __syncthreads();
-    if (tid < 64) {
-        int count = 0;
-        for (int i0 = last + 1; i0 < d.n && !s_leaf; i0 += 64) {
-            const int i = i0 + tid;
-            const bool mine = i < d.n && s_parent[i] == last && !s_dull[i];
-            const uint64_t m = __ballot(mine);
-            if (mine) refusal[count + __popcll(m & ((uint64_t(1) << tid) - 1))] = s_token[i];
-            count += __popcll(m);
+    if constexpr (!kDraft) {
+        // the tokens refused there, each once
+        int* const refusal = s_best;
+        __syncthreads();
+        if (tid < 64) {
+            int count = 0;
+            for (int i0 = last + 1; i0 < d.n && !s_leaf; i0 += 64) {
+                const int i = i0 + tid;
+                const bool mine = i < d.n && s_parent[i] == last && !s_dull[i];
+                const uint64_t m = __ballot(mine);
+                if (mine) refusal[count + __popcll(m & ((uint64_t(1) << tid) - 1))] = s_token[i];
+                count += __popcll(m);
+            }
+            if (tid == 0) s_last = count;
         }
-        if (tid == 0) s_last = count;
+        __syncthreads();
+        const int next = draw_plain<kType>(a, row_of(a, 0, d.first + last, kSize<kType>),
+                                           a.part[0] + int64_t(d.first + last) * a.parts, p, rate, refusal, s_last,
+                                           a.samples[r], s_table, s_scan, s_pick);
+        if (tid == 0) a.next[r] = next;
     }
-    __syncthreads();
-    const int count = s_last;
-    const Part* const part = a.part[0] + int64_t(d.first + last) * a.parts;
-    auto whole_part = [&](int c) {
-        return part[c].top == -INFINITY ? 0.0 : part[c].sum * exp2_64th(s_table, (double(part[c].top) - double(p.top)) * rate);
-    };
-    auto whole_weight = [&](int v) { return share(logit<kType>(row, v), p.top, rate, 1.0, s_table); };
-    const float sample = a.samples[r];
-    int next = draw(
-        a, sample, s_scan, s_pick,
-        [&](int c) {
-            double x = whole_part(c);
-            for (int j = 0; j < count; ++j)
-                if (refusal[j] / kPart == c) x -= whole_weight(refusal[j]);
-            // what rounding leaves of a part whose weight was refused
-            return x > 0x1p-40 * whole_part(c) ? x : 0.0;
-        },
-        [&](int v) {
-            for (int j = 0; j < count; ++j)
-                if (refusal[j] == v) return 0.0;
-            return whole_weight(v);
-        });
-    if (next < 0) next = draw(a, sample, s_scan, s_pick, whole_part, whole_weight);
-    if (tid == 0) a.next[r] = next;
 }
 
 // ---- residual and draw ---------------------------------------------------------------
+
+__device__ __forceinline__ const Part* parts_of_last(const VerifyArgs& a, int side, int r, int64_t row)
+{
+    return a.last_part[side] ? a.last_part[side] + int64_t(r) * a.parts : a.part[side] + row * a.parts;
+}
 
 // What the last token's row is, and its children with their factors; false: nothing to draw.
 template <int kType>
@@ -644,16 +737,16 @@ __device__ __forceinline__ bool last_row(const VerifyArgs& a, int r, double* tab
     const int mark = a.last[r];
     if (mark < 0) return false;
     fill_table(table);
-    const int at = mark & ~(1 << 30);
+    const int at = mark & ~kLeaf;
     const Drafts d = drafts_of(a, r);
     rate = rate_of(a, r);
     row = d.first + at;
     list_children(a, d, at, kids);
     const int lane = int(threadIdx.x) & 63;
-    count = mark >> 30 & 1 ? 0 : kids.count;
-    p = join(a.part[0] + row * a.parts, a.parts, rate, table, lane, 64);
-    if (count > 0) {
-        q = join(a.part[1] + row * a.parts, a.parts, rate, table, lane, 64);
+    count = mark & kLeaf ? 0 : kids.count;
+    p = join(parts_of_last(a, 0, r, row), a.parts, rate, table, lane, 64);
+    if (count > 0 && a.draft) {
+        q = join(parts_of_last(a, 1, r, row), a.parts, rate, table, lane, 64);
         draft_factors<kType>(a, row_of(a, 1, row, kSize<kType>), q, rate, table, kids);
         // after the last refusal r needs no sum of 1
         for (int j = int(threadIdx.x); j < count; j += int(blockDim.x))
@@ -668,7 +761,7 @@ template <int kType>
 __global__ void __launch_bounds__(kWg) kvx_verify_residual_kernel(const VerifyArgs a)
 {
     constexpr int kV = kVec<kType>;
-    __shared__ double s_table[64];
+    __shared__ double s_table[kTable];
     __shared__ Children s_kids;
     const int groups = (a.parts + kWaves - 1) / kWaves;
     const int r = int(blockIdx.x) / groups, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
@@ -684,9 +777,9 @@ __global__ void __launch_bounds__(kWg) kvx_verify_residual_kernel(const VerifyAr
     const int n = min(kPart, a.vocab - c * kPart);
     double sum = 0.0;
     if (count == 0) {
-        const Part t = a.part[0][row * a.parts + c];
+        const Part t = parts_of_last(a, 0, r, row)[c];
         if (lane == 0 && t.top != -INFINITY)
-            sum = t.sum * exp2_64th(s_table, (double(t.top) - double(p.top)) * rate);
+            sum = t.sum * exp2_256th(s_table, (double(t.top) - double(p.top)) * rate);
     } else {
         const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;
         auto one = [&](float lp, float lq, int v) {
@@ -711,7 +804,7 @@ __global__ void __launch_bounds__(kWg) kvx_verify_residual_kernel(const VerifyAr
 template <int kType>
 __global__ void __launch_bounds__(kWalk) kvx_verify_draw_kernel(const VerifyArgs a)
 {
-    __shared__ double s_table[64], s_scan[kWalk / 64 + 1];
+    __shared__ double s_table[kTable], s_scan[kWalk / 64 + 1];
     __shared__ int s_pick[2];
     __shared__ Children s_kids;
     const int r = int(blockIdx.x);
@@ -721,35 +814,45 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_draw_kernel(const VerifyArgs
     int count;
     if (!last_row<kType>(a, r, s_table, s_kids, p, q, row, rate, count)) return;
     const char* const x = row_of(a, 0, row, kSize<kType>);
-    const char* const y = row_of(a, 1, row, kSize<kType>);
-    const double ip = 1.0 / p.sum, iq = count ? 1.0 / q.sum : 0.0;
+    const Part* const part = parts_of_last(a, 0, r, row);
     const float sample = a.samples[r];
-    const Part* const part = a.part[0] + row * a.parts;
-    auto whole_weight = [&](int v) { return share(logit<kType>(x, v), p.top, rate, 1.0, s_table); };
-    int next = draw(
-        a, sample, s_scan, s_pick, [&](int c) { return a.residual[int64_t(r) * a.parts + c]; },
-        [&](int v) {
-            if (count == 0) return whole_weight(v);
-            return refused(share(logit<kType>(x, v), p.top, rate, ip, s_table),
-                           share(logit<kType>(y, v), q.top, rate, iq, s_table), v, count, a.distinct,
-                           [&](int j) { return s_kids.token[j]; }, [&](int j) { return s_kids.by[j]; },
-                           [&](int j) { return s_kids.left[j]; });
-        });
-    if (next < 0)
+    int next = -1;
+    if (!a.draft) {
+        // each refused token once
+        if (threadIdx.x < 64) {
+            const int lane = int(threadIdx.x);
+            int n = 0;
+            for (int j0 = 0; j0 < count; j0 += 64) {
+                const bool mine = j0 + lane < count && !s_kids.dull[j0 + lane];
+                const uint64_t m = __ballot(mine);
+                if (mine) s_kids.number[n + __popcll(m & ((uint64_t(1) << lane) - 1))] = s_kids.token[j0 + lane];
+                n += __popcll(m);
+            }
+            if (lane == 0) s_kids.count = n;
+        }
+        __syncthreads();
+        next = draw_plain<kType>(a, x, part, p, rate, s_kids.number, s_kids.count, sample, s_table, s_scan, s_pick);
+    } else {
+        const char* const y = row_of(a, 1, row, kSize<kType>);
+        const double ip = 1.0 / p.sum, iq = count ? 1.0 / q.sum : 0.0;
         next = draw(
-            a, sample, s_scan, s_pick,
-            [&](int c) {
-                return part[c].top == -INFINITY ? 0.0
-                                                : part[c].sum * exp2_64th(s_table, (double(part[c].top) - double(p.top)) * rate);
-            },
-            whole_weight);
+            a, sample, s_scan, s_pick, [&](int c) { return a.residual[int64_t(r) * a.parts + c]; },
+            [&](int v) {
+                if (count == 0) return share(logit<kType>(x, v), p.top, rate, 1.0, s_table);
+                return refused(share(logit<kType>(x, v), p.top, rate, ip, s_table),
+                               share(logit<kType>(y, v), q.top, rate, iq, s_table), v, count, a.distinct,
+                               [&](int j) { return s_kids.token[j]; }, [&](int j) { return s_kids.by[j]; },
+                               [&](int j) { return s_kids.left[j]; });
+            });
+        if (next < 0) next = draw_plain<kType>(a, x, part, p, rate, s_kids.number, 0, sample, s_table, s_scan, s_pick);
+    }
     if (threadIdx.x == 0) a.next[r] = next;
 }
 
-int64_t part_groups(const VerifyArgs& a)
+// of `rows` rows, and the draft's
+int64_t part_groups(const VerifyArgs& a, int64_t rows)
 {
-    const int64_t units = int64_t(a.total_tokens) * a.parts * (a.draft ? 2 : 1);
-    return (units + kWaves - 1) / kWaves;
+    return (rows * a.parts * (a.draft ? 2 : 1) + kWaves - 1) / kWaves;
 }
 
 int64_t residual_groups(const VerifyArgs& a) { return int64_t(a.num_requests) * ((a.parts + kWaves - 1) / kWaves); }
@@ -757,23 +860,30 @@ int64_t residual_groups(const VerifyArgs& a) { return int64_t(a.num_requests) * 
 template <int kType>
 int go(const VerifyArgs& a, void* stream)
 {
+    const bool coarse = a.last_part[0] != nullptr;
+    const int64_t R = a.num_requests, N = a.total_tokens;
     int err = 0;
-    if (a.total_tokens > 0) err = launch_kernel(kvx_verify_parts_kernel<kType>, part_groups(a), kWg, stream, a);
+    if (N > 0)
+        err = coarse ? launch_kernel(kvx_verify_parts_kernel<kType, kCoarse>, part_groups(a, N), kWg, stream, a)
+                     : launch_kernel(kvx_verify_parts_kernel<kType, kFine>, part_groups(a, N), kWg, stream, a);
+    if (!err && a.draft && a.parents && N > 0) err = launch_kernel(kvx_verify_siblings_kernel<kType>, N, kWalk, stream, a);
     if (err) return err;
-    if (!a.draft) return launch_kernel(kvx_verify_walk_kernel<kType, false>, a.num_requests, kWalk, stream, a);
-    if (a.parents && a.total_tokens > 0)
-        err = launch_kernel(kvx_verify_siblings_kernel<kType>, a.total_tokens, kWalk, stream, a);
-    if (!err) err = launch_kernel(kvx_verify_walk_kernel<kType, true>, a.num_requests, kWalk, stream, a);
-    if (!err) err = launch_kernel(kvx_verify_residual_kernel<kType>, residual_groups(a), kWg, stream, a);
-    if (!err) err = launch_kernel(kvx_verify_draw_kernel<kType>, a.num_requests, kWalk, stream, a);
+    err = a.draft ? launch_kernel(kvx_verify_walk_kernel<kType, true>, R, kWalk, stream, a)
+                  : launch_kernel(kvx_verify_walk_kernel<kType, false>, R, kWalk, stream, a);
+    if (!err && coarse) err = launch_kernel(kvx_verify_parts_kernel<kType, kLast>, part_groups(a, R), kWg, stream, a);
+    if (!err && a.draft) err = launch_kernel(kvx_verify_residual_kernel<kType>, residual_groups(a), kWg, stream, a);
+    if (!err && (a.draft || coarse)) err = launch_kernel(kvx_verify_draw_kernel<kType>, R, kWalk, stream, a);
     return err;
 }
 
 }  // namespace
 
+bool verify_coarse(int64_t tokens, int32_t vocab, bool draft) { return tokens * vocab * (draft ? 2 : 1) >= 1 << 24; }
+
 double verify_threads(const VerifyArgs& a)
 {
-    double most = std::max(double(part_groups(a)) * kWg, double(a.num_requests) * kWalk);
+    double most = std::max(double(part_groups(a, std::max(a.total_tokens, a.num_requests))) * kWg,
+                           double(a.num_requests) * kWalk);
     if (a.draft) most = std::max(most, double(residual_groups(a)) * kWg);
     if (a.draft && a.parents) most = std::max(most, double(a.total_tokens) * kWalk);
     return most;

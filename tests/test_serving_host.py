@@ -70,7 +70,7 @@ def test_fetch_is_refused():
         assert fetch(b=host.batch(**over)) == K.EINVAL
     assert fetch(b=host.batch(total_tokens=0), k=None) == K.OK
     assert fetch(c=host.cache(num_requests=0), k=None) == K.OK
-    assert fetch(b=host.batch(total_tokens=1 << 24)) == K.EUNSUPPORTED
+    assert fetch(b=host.batch(total_tokens=1 << 28)) == K.EUNSUPPORTED
 
 
 @pytest.mark.parametrize("over", [

@@ -138,7 +138,7 @@ typedef struct {
  *            q_heads 0: keys and values only.
  * Values are turned in fp32 and rounded once: q to dtype, k and v to the
  * cache's type (to nearest even; an 8-bit cache takes the casts of kvx.h, its
- * scale from the fp32 row).  Tokens whose slot has no page write no row.  A 16-bit
+ * scale from the fp32 row, a 4-bit one KVX_FP4_E2M1's).  Tokens whose slot has no page write no row.  A 16-bit
  * cache may have the other 16-bit type than k and v; kvx_attend and kvx_weigh then
  * take queries of the cache's type.
  * KVX_EINVAL: NULL or misaligned pointers, sizes out of the ranges above, layer
@@ -162,7 +162,8 @@ kvx_status kvx_append(const kvx_cache *cache, const kvx_batch *batch, const kvx_
  * count).  What lies in slots that a token does not see (infinities and NaN too) has
  * no part in its result.  Scores, softmax statistics and sums are fp32.  For the
  * product with V weights are rounded to 16 bits, with max_tokens * q_heads / Hd <= 16
- * to twice as many; the output is rounded once to dtype.  A 16-bit cache must have
+ * to twice as many; over a 4-bit cache both products are of bf16, fp16 queries and
+ * their weights in two such terms; the output is rounded once to dtype.  A 16-bit cache must have
  * the type of q (KVX_EUNSUPPORTED otherwise); q_heads is a multiple of Hd with at
  * most 1024 query heads per KV head. */
 kvx_status kvx_attend(const kvx_cache *cache, const kvx_batch *batch, const kvx_scores *scores,
@@ -180,7 +181,8 @@ kvx_status kvx_attend_workspace(const kvx_cache *cache, const kvx_batch *batch, 
  * of the slots that it sees NaN).
  *   weights: device fp32 [num_requests][Hd][w_stride], w_stride >= max_context:
  *            slots j < C_r have the sum added, the new tokens' slots are set to
- *            it, others are not touched. */
+ *            it, others are not touched.
+ * KVX_EUNSUPPORTED: a 4-bit cache, and as kvx_attend. */
 kvx_status kvx_weigh(const kvx_cache *cache, const kvx_batch *batch, const kvx_scores *scores,
                      int32_t layer, int32_t dtype, int32_t q_heads, const void *q,
                      int64_t q_stride, const float *lse, float *weights, int64_t w_stride,

@@ -787,18 +787,16 @@ int join(const AttendArgs& a, const AttendPlan& p, void* stream)
 
 void plan_few_fp4(const kvx_cache& c, const kvx_batch& b, AttendPlan& p)
 {
-    // Heads of a workgroup: as many as leave every column its twin, up to 256 elements; fewer where the
-    // card is not full without.
-    const int64_t turns = (int64_t(b.max_context) + kStep - 1) / kStep;
-    const bool short_ones = turns <= 8;                // a workgroup to each request's pack
+    // Heads of a workgroup: as many as leave every column its twin, up to 256 elements.
     p.heads = c.head_dim > 128 ? 1 : c.head_dim > 64 ? 2 : 4;
-    while (p.heads > 1 && (c.num_kv_heads % p.heads || p.rows * p.heads > 8 ||
-                           (short_ones && int64_t(c.num_requests) * (c.num_kv_heads / p.heads) < 256)))
-        p.heads >>= 1;
+    while (p.heads > 1 && (c.num_kv_heads % p.heads || p.rows * p.heads > 8)) p.heads >>= 1;
+    // A workgroup to each request's pack: short ones, and so many that the card evens them out and
+    // finding a range's place among them would cost; fewer heads to each where they do not fill the card.
+    const int64_t requests = c.num_requests, turns = (int64_t(b.max_context) + kStep - 1) / kStep;
+    const bool single = turns <= 8 || requests >= 512 || requests * (c.num_kv_heads / p.heads) >= 1024;
+    while (single && p.heads > 1 && requests * (c.num_kv_heads / p.heads) < 256) p.heads >>= 1;
     // two workgroups to a CU
-    p.ranges = short_ones ? 0
-                          : int(std::max<int64_t>(1, std::min<int64_t>(512 / (c.num_kv_heads / p.heads),
-                                                                       c.num_requests * turns / 2)));
+    p.ranges = single ? 0 : int(std::max<int64_t>(1, std::min<int64_t>(512 / (c.num_kv_heads / p.heads), requests * turns / 2)));
 }
 
 uint64_t workspace_fp4(const kvx_cache& c, const AttendPlan& p)

@@ -173,21 +173,22 @@ AttendPlan attend_plan(const kvx_cache& c, const kvx_batch& b, int32_t q_heads)
     const bool eight_bit = c.dtype == KVX_FP8_E4M3FN || c.dtype == KVX_FP8_E5M2;
     const int64_t heads = int64_t(c.num_requests) * c.num_kv_heads;
     const int64_t pieces = heads * ((b.max_context + 1023) / 1024);
+    // A 4-bit cache has a few-rows kernel of its own, which numbers a plane's groups with 32 bits.
+    const bool four_bit = c.dtype == KVX_FP4_E2M1;
+    if (four_bit && p.rows <= 16 &&
+        double(c.num_blocks) * c.block_size * c.num_kv_heads * (c.head_dim / 32) < 0x1p32) {
+        p.few = true;
+        plan_few_fp4(c, b, p);
+        return p;
+    }
     // 17 to 32 rows: the few-rows kernel's registers do not hold more than 128 elements; it cuts
     // the slots finer, which serves small calls (32 query heads on one KV head, one request of 8000
     // slots: 17 us, 39 with the other kernel; trees of 4..8 nodes over an fp8 cache of 2048..16384
     // slots: 128, 133), and where a 16-bit cache's slots fill the card in any case the other kernel
     // reads them faster (the same trees, 64 of them, bf16: 330 us, 362 with this one; at 512 pieces
     // both take 48).
-    // that kernel numbers a plane's groups with 32 bits
-    if (c.dtype == KVX_FP4_E2M1 && p.rows <= 16 &&
-        double(c.num_blocks) * c.block_size * c.num_kv_heads * (c.head_dim / 32) < 0x1p32) {
-        p.few = true;
-        plan_few_fp4(c, b, p);
-        return p;
-    }
-    p.few = p.rows <= 16 || (p.rows <= 32 && c.head_dim <= 128 && c.dtype != KVX_FP4_E2M1 &&
-                             (eight_bit || pieces < 512));
+    p.few = !four_bit && (p.rows <= 16 || (p.rows <= 32 && c.head_dim <= 128 &&
+                                           (eight_bit || pieces < 512)));
     p.tile_rows = p.few ? (p.rows <= 16 ? 16 : 32) : p.rows <= 64 ? 64 : 128;
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     if (p.few) {

@@ -126,6 +126,37 @@ def test_good_calls_reach_the_device():
     assert host.evict(c=four()) == K.EDEVICE
 
 
+@pytest.mark.parametrize("requests,context", [(1, 100), (3, 100), (3, 16384), (600, 16384)])
+@pytest.mark.parametrize("over", [dict(), dict(head_dim=256), dict(num_kv_heads=1), dict(num_kv_heads=7, head_dim=96)],
+                         ids=str)
+def test_attend_plans_of_a_four_bit_cache(requests, context, over):
+    """The sums of ranges hold a row of statistics and elements each; planes of more groups than 32 bits
+    number are for the other kernel, whose sums are of splits."""
+    shape = dict(num_requests=requests, bt_stride=1024, **over)
+    heads = 4 * shape.get("num_kv_heads", 4)
+    b = host.batch(total_tokens=requests, max_tokens=1, max_context=context)
+    nbytes = ctypes.c_uint64()
+
+    def workspace(c):
+        assert K._lib.kvx_attend_workspace(c.ref, b.ref, heads, ctypes.byref(nbytes)) == K.OK
+        return nbytes.value
+
+    small, large = four(**shape), four(num_blocks=1 << 32, **shape)
+    dim = shape.get("head_dim", 64)
+    if context == 100 or requests >= 512:
+        assert workspace(small) == 0             # a workgroup to each
+    else:
+        assert workspace(small) >= 16 * (2 + dim) * 4 and workspace(small) < 1 << 27
+    splits = workspace(large) / (4 * ((requests * heads + 3) // 4) * (2 + dim) * 4)
+    filled = requests * heads // 4 >= 768        # with a workgroup to each
+    assert splits == int(splits) and (splits == 0) == (context == 100 or filled)
+    for c in (small, large):
+        if workspace(c):
+            assert host.attend(c=c, b=b, heads=heads, qs=heads * dim, os_=heads * dim, nbytes=nbytes.value - 1) == K.EINVAL
+        if torch.cuda.device_count() == 0:
+            assert host.attend(c=c, b=b, heads=heads, qs=heads * dim, os_=heads * dim) == K.EDEVICE
+
+
 def test_binding_refuses_layouts():
     table = torch.zeros((1, 4), dtype=torch.int32)
     codes = torch.zeros((1, 2, 3, 16, 2, 32), dtype=torch.uint8)

@@ -16,7 +16,7 @@
 //                 one.  More columns take single elements, which v_perm_b32 puts together.  The
 //                 result rows belong to the heads of their m; what they hold in columns of
 //                 other heads is left.
-// The slots' places and scale bytes are looked up 3072 at a time into LDS, the latter while the
+// The slots' places and scale bytes are looked up 2816 at a time into LDS, the latter while the
 // first rows are on their way; a tile's rows are for the whole of the turn before.  Codes are
 // finite whatever they are; a value's group that is NaN counts as zero in the products, and
 // where there was one a walk over the slots says which rows saw it.
@@ -45,7 +45,7 @@ constexpr int kWaves = 4;
 constexpr int kWg = 64 * kWaves;
 constexpr int kTile = 32;           // slots of a wave's turn
 constexpr int kStep = kWaves * kTile;   // of a workgroup's
-constexpr int kChunk = 3072;        // slots whose places and scale bytes are in LDS at once
+constexpr int kChunk = 22 * kStep;  // slots whose places and scale bytes are in LDS at once
 
 template <int DP, int HP, bool kDup>
 struct Shape {
@@ -350,6 +350,7 @@ __global__ void __launch_bounds__(kWg, 2) kvx_attend_fp4_kernel(const AttendArgs
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int at = from - c0 + k * kWg + tid;
+                if (at >= kChunk) break;               // whole waves
                 const uint64_t some = __ballot(row[k] >= 0);
                 if (lane == 0) s_valid[at >> 6] = some;
                 s_at[at] = row[k] < 0 ? 0u : uint32_t((row[k] + h0) * rg);

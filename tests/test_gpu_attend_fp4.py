@@ -99,6 +99,23 @@ def test_splits(K, dim, heads, group, shape):
     check(p, out, lse)
 
 
+@pytest.mark.parametrize("requests,heads,group,dim,longest", [(511, 1, 4, 64, 1500), (512, 1, 4, 64, 1500),
+                                                              (127, 8, 8, 32, 1100), (128, 8, 8, 32, 1100),
+                                                              (1, 8, 4, 128, 1024), (1, 8, 4, 128, 1025)])
+def test_many_requests(K, requests, heads, group, dim, longest):
+    """On both sides of where every request has workgroups of its own, some of them longer than a
+    workgroup's list of places, some empty."""
+    g = torch.Generator().manual_seed(requests)
+    ctx = torch.randint(0, longest, (requests,), generator=g).tolist()
+    new = torch.randint(0, 2, (requests,), generator=g).tolist()
+    ctx[0], new[0] = longest - 1, 1
+    if requests > 2:
+        ctx[-1], new[-1], ctx[1], new[1] = 6000, 1, 0, 1
+    p = Problem(new=new, ctx=ctx, heads=heads, group=group, dim=dim, seed=requests)
+    out, lse, _ = run(K, p)
+    check(p, out, lse)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("new", [[1, 1, 1], [4, 2, 1], [30, 20, 9]], ids=str)
 def test_rows_far_apart(K, dtype, new):

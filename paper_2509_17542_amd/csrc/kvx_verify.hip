@@ -597,7 +597,7 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_walk_kernel(const VerifyArgs
         if (tid == 0) {
             a.counts[r] = 0;
             a.next[r] = -1;
-            if constexpr (kDraft) a.last[r] = -1;
+            if (a.last) a.last[r] = -1;
         }
         return;
     }

@@ -244,6 +244,24 @@ def test_largest_request(K, kind):
     p.check(K)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+def test_many_logits(K, kind, dtype):
+    """17 million logits, whose last rows are summed again: requests without tokens (whose share of the
+    workspace nobody fills), greedy and nearly greedy ones, paths cut, rows that are no distribution."""
+    new = [5, 0, 9, 16, 0, 2, 1, 30, 24, 28, 0]
+    t = [1.0, 1.0, 0.0, 0.5, 0.7, 2.0, 0.0, 1.0, 1e-12, 0.9, 1.0]
+    p = Problem(new, vocab=150001, dtype=dtype, seed=21, near=0.98, peak=15.0, temperatures=t, shift=1, **kind)
+    assert p.logits.numel() >= 1 << 24
+    p.check(K)
+    p.check(K, a_stride=2)
+    for x in (p.logits, p.d_logits):
+        x[p.starts[3]] = -math.inf
+        x[p.starts[7], 77] = math.nan
+        x[p.starts[9], 5:] = -math.inf
+    p.check(K)
+
+
 def test_wide_star(K):
     """Hundreds of children of one token."""
     for draft in (False, True):

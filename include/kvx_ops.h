@@ -153,7 +153,8 @@ kvx_status kvx_append(const kvx_cache *cache, const kvx_batch *batch, const kvx_
  *   q, out:    dtype, layout and strides as above.
  *   lse:       device fp32 [N][q_heads] or NULL: log of the sum of exp(x).
  *   workspace: device, >= kvx_attend_workspace bytes, 16-byte aligned; NULL if
- *              that is 0.  Its contents need not be kept between calls.
+ *              that is 0.  Its contents need not be kept between calls; calls (and graphs)
+ *              that may run at the same time need one each.
  * A token that sees no slot, or whose scores are all -infinity, gives zeros and an
  * lse of -infinity; a NaN among its scores (from q or from a key that it sees)
  * gives NaN in both.  An infinite value in a slot that it sees makes that element of

@@ -225,10 +225,12 @@ __global__ void __launch_bounds__(kWg, (kPass == kCoarse ? 6 : 4)) kvx_verify_pa
     int first = INT32_MAX;
     if (rate == 0.0) {
 #pragma unroll
-        for (int k = 0; k < kEach; ++k)
+        for (int k = 0; k < kEach; ++k) {
+            const int from = max(min((k * 64 + lane) * kV, n - kV), 0);   // where its 16 bytes lie
 #pragma unroll
             for (int e = 0; e < kV; ++e)
-                if (element<kType>(w[k], e) == top) first = min(first, c * kPart + (k * 64 + lane) * kV + e);
+                if (element<kType>(w[k], e) == top) first = min(first, c * kPart + from + e);
+        }
         for (int o = 32; o; o >>= 1) first = min(first, __shfl_xor(first, o));
     }
     double sum = 0.0;

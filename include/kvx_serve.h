@@ -89,7 +89,7 @@ typedef struct {
  *   next_tokens: device int32 [R]; -1 where there is none.
  *   workspace: device, >= kvx_verify_workspace bytes, 16-byte aligned; calls (and graphs) that may
  *              run at the same time need one each.
- * What the next token is drawn by is summed in 64 bits, from exponentials of 1e-13.  So is
+ * What the next token is drawn by is summed in 64 bits, from exponentials of 2e-13.  So is
  * what tokens are accepted by where the logits (the draft's too) are fewer than 2^24; from
  * there on its exponentials are fp32, its sums 64-bit.  A row that has a NaN or +infinity, or nothing
  * but -infinity, is no distribution: after it all children are refused, and there is

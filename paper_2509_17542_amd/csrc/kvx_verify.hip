@@ -13,7 +13,7 @@
 //   draw      the part by the parts' sums, the token by a scan over that part.
 // The next token is the place where a sum over up to V terms passes a given share of
 // the whole: an error of 1e-7 of it, as of fp32 exponentials, moves thousands of such
-// borders by that much, so what it goes by is summed in 64 bits, from exponentials of 1e-13.
+// borders by that much, so what it goes by is summed in 64 bits, from exponentials of 2e-13.
 // Whether a token is accepted is one comparison, which fp32 exponentials decide otherwise
 // once in 10^7: from 2^24 logits on all rows are summed from those (80 million logits of bf16: 41 us, 4
 // TB/s; 68 in 64 bits) and the last rows in 64 bits again (17 million: 15 us); fewer are in 64 bits at
@@ -65,7 +65,7 @@ __device__ __forceinline__ u32x4 load16(const char* p)
     return w;
 }
 
-// exp2(x / 256) to 1e-13, -2.6e5 <= x <= 256; x = 256 n + j + f, |f| <= 1/2: 2^(j / 256) out of
+// exp2(x / 256) to 1.5e-13, -2.6e5 <= x <= 256; x = 256 n + j + f, |f| <= 1/2: 2^(j / 256) out of
 // a table, the series of exp(f ln 2 / 256), whose first term left out is (ln 2 / 512)^4 / 24, and
 // n added to the exponent.  Adding 1.5 x 2^52 rounds x to an integer, which lies in the low word.
 constexpr int kTable = 256;
@@ -95,13 +95,12 @@ __device__ __forceinline__ void fill_table(double* table)
     for (int i = int(threadIdx.x); i < kTable; i += int(blockDim.x)) table[i] = exp2(double(i) / kTable);
 }
 
-// 256 log2(e) / T, of 40 bits: its products with 16-bit logits are exact.  0: greedy
+// 256 log2(e) / T.  0: greedy
 __device__ __forceinline__ double rate_of(const VerifyArgs& a, int r)
 {
     const float t = a.temperatures ? a.temperatures[r] : 1.0f;
     if (!(t >= 0x1p-60f)) return 0.0;
-    const double rate = 369.32993046757462751 / double(fminf(t, 0x1p60f));
-    return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, rate) & ~uint64_t(0x1FFF));
+    return 369.32993046757462751 / double(fminf(t, 0x1p60f));
 }
 
 struct Drafts {
@@ -257,14 +256,14 @@ __global__ void __launch_bounds__(kWg, (kPass == kCoarse ? 6 : 4)) kvx_verify_pa
             sum += double(x[0]);
         }
     } else {
-        // what is far below weighs 2^-976 here
-        const double back = -double(top) * rate;
+        // What is far below weighs 2^-976 here.  The difference is formed first: a multiply-add of the
+        // product and top's would save an instruction, but takes a rate cut to 40 bits, 1e-12 of the
+        // distance from the top.
 #pragma unroll
         for (int k = 0; k < kEach; ++k)
 #pragma unroll
             for (int e = 0; e < kV; ++e) {
-                const double v = double(element<kType>(w[k], e));
-                const double x = kType == kF32 ? (v - double(top)) * rate : __builtin_fma(v, rate, back);
+                const double x = (double(element<kType>(w[k], e)) - double(top)) * rate;
                 sum += exp2_near(s_table, fmax(x, kLeast));
             }
     }

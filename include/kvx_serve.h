@@ -89,9 +89,8 @@ typedef struct {
  *   next_tokens: device int32 [R]; -1 where there is none.
  *   workspace: device, >= kvx_verify_workspace bytes, 16-byte aligned; calls (and graphs) that may
  *              run at the same time need one each.
- * What the next token is drawn by is summed in 64 bits, from exponentials of 2e-13.  So is
- * what tokens are accepted by where the logits (the draft's too) are fewer than 2^24; from
- * there on its exponentials are fp32, its sums 64-bit.  A row that has a NaN or +infinity, or nothing
+ * What tokens are accepted by and the next one is drawn by is summed in 64 bits, from
+ * exponentials of 2e-13; it does not depend on the other requests of the call.  A row that has a NaN or +infinity, or nothing
  * but -infinity, is no distribution: after it all children are refused, and there is
  * no next token; where the draft's row is none, its children are refused and the next
  * token is drawn from p.

@@ -39,16 +39,11 @@ uint64_t place(const kvx_drafts& d, bool draft, char* base, kvx::VerifyArgs& a)
     };
     const uint64_t N = d.total_tokens, R = d.num_requests, C = parts_of(d);
     a.part[0] = reinterpret_cast<kvx::Part*>(take(N * C * sizeof(kvx::Part)));
-    const bool coarse = kvx::verify_coarse(d.total_tokens, d.vocab, draft);
-    if (coarse) {
-        for (int side = 0; side < (draft ? 2 : 1); ++side)
-            a.last_part[side] = reinterpret_cast<kvx::Part*>(take(R * C * sizeof(kvx::Part)));
-    }
-    if (draft || coarse) a.last = reinterpret_cast<int32_t*>(take(R * 4));
     if (draft) {
         a.part[1] = reinterpret_cast<kvx::Part*>(take(N * C * sizeof(kvx::Part)));
         a.left = reinterpret_cast<double*>(take(N * 8));
         a.residual = reinterpret_cast<double*>(take(R * C * 8));
+        a.last = reinterpret_cast<int32_t*>(take(R * 4));
     }
     return at;
 }

@@ -7,18 +7,17 @@
 //             another child may follow;
 //   walk      a workgroup per request joins its rows' parts, decides for every token
 //             whether its parent would accept it (that does not depend on the path), and
-//             follows the path from the first;
-//   last      (many logits) the parts of the rows after which the next tokens are drawn, again;
-//   residual  (draft's logits given) the sums of max(r - q, 0) there;
-//   draw      the part by the parts' sums, the token by a scan over that part.
+//             follows the path from the first; without a draft it draws the next token too:
+//             the part by the parts' sums, the token by a scan over that part;
+//   residual  (draft's logits given) the sums of max(r - q, 0) after the last token;
+//   draw      (draft's logits given) the next token by those.
 // The next token is the place where a sum over up to V terms passes a given share of
 // the whole: an error of 1e-7 of it, as of fp32 exponentials, moves thousands of such
-// borders by that much, so what it goes by is summed in 64 bits, from exponentials of 2e-13.
-// Whether a token is accepted is one comparison, which fp32 exponentials decide otherwise
-// once in 10^7: from 2^24 logits on all rows are summed from those (80 million logits of bf16: 41 us, 4
-// TB/s; 68 in 64 bits) and the last rows in 64 bits again (17 million: 15 us); fewer are in 64 bits at
-// once, which saves two launches.  64 chains of 2..9 tokens over 128256 logits with a draft's take 108 us,
-// four tokens over 32000 logits 21, nearly all of it launches and chains of lookups.
+// borders by that much, so all sums are of 64 bits, from exponentials of 2e-13, and a
+// request has the same answer in a call of any size.  80 million logits of bf16 take 68 us, 2.4
+// TB/s (41 with fp32 exponentials, summed eight at a time in fp32).
+// 64 chains of 2..9 tokens over 128256 logits with a draft's take 123 us, four tokens over 32000
+// logits 21, nearly all of it launches and chains of lookups.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -138,31 +137,24 @@ __device__ __forceinline__ const char* row_of(const VerifyArgs& a, int side, int
 
 constexpr int kLeaf = 1 << 30;           // VerifyArgs::last: nothing was refused there
 
-enum Pass : int { kFine = 0, kCoarse = 1, kLast = 2 };
-
-template <int kType, int kPass>
-__global__ void __launch_bounds__(kWg, (kPass == kCoarse ? 6 : 4)) kvx_verify_parts_kernel(const VerifyArgs a)
+template <int kType>
+__global__ void __launch_bounds__(kWg, 4) kvx_verify_parts_kernel(const VerifyArgs a)
 {
     constexpr int kV = kVec<kType>, kEach = kPart / 64 / kV;
-    __shared__ double s_table[kPass == kCoarse ? 1 : kTable];
-    if constexpr (kPass != kCoarse) {
-        fill_table(s_table);
-        __syncthreads();
-    }
+    __shared__ double s_table[kTable];
+    fill_table(s_table);
+    __syncthreads();
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int64_t unit = int64_t(blockIdx.x) * kWaves + wave, rows = unit / a.parts;
-    const int32_t of = kPass == kLast ? a.num_requests : a.total_tokens;
-    const int c = int(unit - rows * a.parts), side = rows >= of, index = int(rows - (side ? of : 0));
-    if (index >= of || (side && !a.draft)) return;
-    const int mark = kPass == kLast ? a.last[index] : 0;
-    if (mark < 0) return;
-    const int r = kPass == kLast ? index : request_at(a.starts, a.num_requests, index);
+    const int c = int(unit - rows * a.parts), side = rows >= a.total_tokens;
+    const int64_t index = rows - (side ? a.total_tokens : 0);
+    if (index >= a.total_tokens || (side && !a.draft)) return;
+    const int row = int(index), r = request_at(a.starts, a.num_requests, row);
     if (r < 0 || r >= a.num_requests) return;
     const Drafts d = drafts_of(a, r);
-    const int at = kPass == kLast ? mark & ~kLeaf : index - d.first, row = d.first + at;
+    const int at = row - d.first;
     if (at >= d.n) return;
     const double rate = rate_of(a, r);
-    if (kPass == kLast && side && mark & kLeaf) return;
     if (side) {
         // a draft's row counts where it has children
         bool some = false;
@@ -237,24 +229,6 @@ __global__ void __launch_bounds__(kWg, (kPass == kCoarse ? 6 : 4)) kvx_verify_pa
         sum = 0.0;
     } else if (rate == 0.0) {
         sum = lane == 0 ? 1.0 : 0.0;
-    } else if constexpr (kPass == kCoarse) {
-        // log2(e) / T in two terms; differences of 200 in log2 and more are 0
-        const double by = rate * (1.0 / kTable);
-        const float hi = float(by), lo = float(by - double(hi)), least = -200.0f / hi;
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            float x[kV];
-#pragma unroll
-            for (int e = 0; e < kV; ++e) {
-                const float d = fmaxf(element<kType>(w[k], e) - top, least);
-                x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, hi, d * lo));
-            }
-#pragma unroll
-            for (int n = kV / 2; n; n >>= 1)
-#pragma unroll
-                for (int e = 0; e < n; ++e) x[e] += x[e + n];
-            sum += double(x[0]);
-        }
     } else {
         // What is far below weighs 2^-976 here.  The difference is formed first: a multiply-add of the
         // product and top's would save an instruction, but takes a rate cut to 40 bits, 1e-12 of the
@@ -269,8 +243,7 @@ __global__ void __launch_bounds__(kWg, (kPass == kCoarse ? 6 : 4)) kvx_verify_pa
     }
     sum = wave_sum(sum);
     if (bad) sum = NAN;
-    Part* const out = kPass == kLast ? a.last_part[side] + int64_t(r) * a.parts : a.part[side] + int64_t(row) * a.parts;
-    if (lane == 0) out[c] = Part{sum, top, first};
+    if (lane == 0) a.part[side][int64_t(row) * a.parts + c] = Part{sum, top, first};
 }
 
 // ---- what a row is ---------------------------------------------------------------
@@ -417,8 +390,8 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_siblings_kernel(const Verify
     const int count = s_kids.count;
     if (count < 2) return;
     const int lane = int(threadIdx.x) & 63;
-    Whole p = join(a.part[0] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
-    Whole q = join(a.part[1] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
+    const Whole p = join(a.part[0] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
+    const Whole q = join(a.part[1] + int64_t(row) * a.parts, a.parts, rate, s_table, lane, 64);
     if (p.sum == 0.0 || q.sum == 0.0) return;
     const char* const pr = row_of(a, 0, row, kSize<kType>);
     const char* const qr = row_of(a, 1, row, kSize<kType>);
@@ -435,15 +408,6 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_siblings_kernel(const Verify
             }
         }
     };
-    if (a.last_part[0]) {                // the parts' sums are of fp32 exponentials
-        double sp = 0.0, sq = 0.0;
-        walk([&](float lp, float lq, int) {
-            sp += share(lp, p.top, rate, 1.0, s_table);
-            sq += share(lq, q.top, rate, 1.0, s_table);
-        });
-        p.sum = group_sum<kWalk>(sp, s_part);
-        q.sum = group_sum<kWalk>(sq, s_part);
-    }
     draft_factors<kType>(a, qr, q, rate, s_table, s_kids);
     const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;
     for (int k = 0; k + 1 < count; ++k) {
@@ -598,7 +562,7 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_walk_kernel(const VerifyArgs
         if (tid == 0) {
             a.counts[r] = 0;
             a.next[r] = -1;
-            if (a.last) a.last[r] = -1;
+            if constexpr (kDraft) a.last[r] = -1;
         }
         return;
     }
@@ -692,17 +656,14 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_walk_kernel(const VerifyArgs
     if (p.sum == 0.0 || rate == 0.0) {
         if (tid == 0) {
             a.next[r] = p.sum == 0.0 ? -1 : p.at;
-            if (a.last) a.last[r] = -1;
+            if constexpr (kDraft) a.last[r] = -1;
         }
         return;
     }
-    if (kDraft || a.last) {
-        bool leaf = s_leaf;
-        if constexpr (kDraft) leaf |= s_row[1][last].sum == 0.0;
+    if constexpr (kDraft) {
+        const bool leaf = s_leaf || s_row[1][last].sum == 0.0;
         if (tid == 0) a.last[r] = last | (leaf ? kLeaf : 0);
-        return;
-    }
-    if constexpr (!kDraft) {
+    } else {
         // the tokens refused there, each once
         int* const refusal = s_best;
         __syncthreads();
@@ -727,11 +688,6 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_walk_kernel(const VerifyArgs
 
 // ---- residual and draw ---------------------------------------------------------------
 
-__device__ __forceinline__ const Part* parts_of_last(const VerifyArgs& a, int side, int r, int64_t row)
-{
-    return a.last_part[side] ? a.last_part[side] + int64_t(r) * a.parts : a.part[side] + row * a.parts;
-}
-
 // What the last token's row is, and its children with their factors; false: nothing to draw.
 template <int kType>
 __device__ __forceinline__ bool last_row(const VerifyArgs& a, int r, double* table, Children& kids, Whole& p, Whole& q,
@@ -747,9 +703,9 @@ __device__ __forceinline__ bool last_row(const VerifyArgs& a, int r, double* tab
     list_children(a, d, at, kids);
     const int lane = int(threadIdx.x) & 63;
     count = mark & kLeaf ? 0 : kids.count;
-    p = join(parts_of_last(a, 0, r, row), a.parts, rate, table, lane, 64);
-    if (count > 0 && a.draft) {
-        q = join(parts_of_last(a, 1, r, row), a.parts, rate, table, lane, 64);
+    p = join(a.part[0] + row * a.parts, a.parts, rate, table, lane, 64);
+    if (count > 0) {
+        q = join(a.part[1] + row * a.parts, a.parts, rate, table, lane, 64);
         draft_factors<kType>(a, row_of(a, 1, row, kSize<kType>), q, rate, table, kids);
         // after the last refusal r needs no sum of 1
         for (int j = int(threadIdx.x); j < count; j += int(blockDim.x))
@@ -780,7 +736,7 @@ __global__ void __launch_bounds__(kWg) kvx_verify_residual_kernel(const VerifyAr
     const int n = min(kPart, a.vocab - c * kPart);
     double sum = 0.0;
     if (count == 0) {
-        const Part t = parts_of_last(a, 0, r, row)[c];
+        const Part t = a.part[0][row * a.parts + c];
         if (lane == 0 && t.top != -INFINITY)
             sum = t.sum * exp2_256th(s_table, (double(t.top) - double(p.top)) * rate);
     } else {
@@ -817,45 +773,27 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_draw_kernel(const VerifyArgs
     int count;
     if (!last_row<kType>(a, r, s_table, s_kids, p, q, row, rate, count)) return;
     const char* const x = row_of(a, 0, row, kSize<kType>);
-    const Part* const part = parts_of_last(a, 0, r, row);
+    const char* const y = row_of(a, 1, row, kSize<kType>);
     const float sample = a.samples[r];
-    int next = -1;
-    if (!a.draft) {
-        // each refused token once
-        if (threadIdx.x < 64) {
-            const int lane = int(threadIdx.x);
-            int n = 0;
-            for (int j0 = 0; j0 < count; j0 += 64) {
-                const bool mine = j0 + lane < count && !s_kids.dull[j0 + lane];
-                const uint64_t m = __ballot(mine);
-                if (mine) s_kids.number[n + __popcll(m & ((uint64_t(1) << lane) - 1))] = s_kids.token[j0 + lane];
-                n += __popcll(m);
-            }
-            if (lane == 0) s_kids.count = n;
-        }
-        __syncthreads();
-        next = draw_plain<kType>(a, x, part, p, rate, s_kids.number, s_kids.count, sample, s_table, s_scan, s_pick);
-    } else {
-        const char* const y = row_of(a, 1, row, kSize<kType>);
-        const double ip = 1.0 / p.sum, iq = count ? 1.0 / q.sum : 0.0;
-        next = draw(
-            a, sample, s_scan, s_pick, [&](int c) { return a.residual[int64_t(r) * a.parts + c]; },
-            [&](int v) {
-                if (count == 0) return share(logit<kType>(x, v), p.top, rate, 1.0, s_table);
-                return refused(share(logit<kType>(x, v), p.top, rate, ip, s_table),
-                               share(logit<kType>(y, v), q.top, rate, iq, s_table), v, count, a.distinct,
-                               [&](int j) { return s_kids.token[j]; }, [&](int j) { return s_kids.by[j]; },
-                               [&](int j) { return s_kids.left[j]; });
-            });
-        if (next < 0) next = draw_plain<kType>(a, x, part, p, rate, s_kids.number, 0, sample, s_table, s_scan, s_pick);
-    }
+    const double ip = 1.0 / p.sum, iq = count ? 1.0 / q.sum : 0.0;
+    int next = draw(
+        a, sample, s_scan, s_pick, [&](int c) { return a.residual[int64_t(r) * a.parts + c]; },
+        [&](int v) {
+            if (count == 0) return share(logit<kType>(x, v), p.top, rate, 1.0, s_table);
+            return refused(share(logit<kType>(x, v), p.top, rate, ip, s_table),
+                           share(logit<kType>(y, v), q.top, rate, iq, s_table), v, count, a.distinct,
+                           [&](int j) { return s_kids.token[j]; }, [&](int j) { return s_kids.by[j]; },
+                           [&](int j) { return s_kids.left[j]; });
+        });
+    if (next < 0)
+        next = draw_plain<kType>(a, x, a.part[0] + row * a.parts, p, rate, s_kids.number, 0, sample, s_table, s_scan, s_pick);
     if (threadIdx.x == 0) a.next[r] = next;
 }
 
-// of `rows` rows, and the draft's
-int64_t part_groups(const VerifyArgs& a, int64_t rows)
+// of all rows, the draft's too
+int64_t part_groups(const VerifyArgs& a)
 {
-    return (rows * a.parts * (a.draft ? 2 : 1) + kWaves - 1) / kWaves;
+    return (int64_t(a.total_tokens) * a.parts * (a.draft ? 2 : 1) + kWaves - 1) / kWaves;
 }
 
 int64_t residual_groups(const VerifyArgs& a) { return int64_t(a.num_requests) * ((a.parts + kWaves - 1) / kWaves); }
@@ -863,30 +801,23 @@ int64_t residual_groups(const VerifyArgs& a) { return int64_t(a.num_requests) * 
 template <int kType>
 int go(const VerifyArgs& a, void* stream)
 {
-    const bool coarse = a.last_part[0] != nullptr;
     const int64_t R = a.num_requests, N = a.total_tokens;
     int err = 0;
-    if (N > 0)
-        err = coarse ? launch_kernel(kvx_verify_parts_kernel<kType, kCoarse>, part_groups(a, N), kWg, stream, a)
-                     : launch_kernel(kvx_verify_parts_kernel<kType, kFine>, part_groups(a, N), kWg, stream, a);
+    if (N > 0) err = launch_kernel(kvx_verify_parts_kernel<kType>, part_groups(a), kWg, stream, a);
     if (!err && a.draft && a.parents && N > 0) err = launch_kernel(kvx_verify_siblings_kernel<kType>, N, kWalk, stream, a);
     if (err) return err;
-    err = a.draft ? launch_kernel(kvx_verify_walk_kernel<kType, true>, R, kWalk, stream, a)
-                  : launch_kernel(kvx_verify_walk_kernel<kType, false>, R, kWalk, stream, a);
-    if (!err && coarse) err = launch_kernel(kvx_verify_parts_kernel<kType, kLast>, part_groups(a, R), kWg, stream, a);
-    if (!err && a.draft) err = launch_kernel(kvx_verify_residual_kernel<kType>, residual_groups(a), kWg, stream, a);
-    if (!err && (a.draft || coarse)) err = launch_kernel(kvx_verify_draw_kernel<kType>, R, kWalk, stream, a);
+    if (!a.draft) return launch_kernel(kvx_verify_walk_kernel<kType, false>, R, kWalk, stream, a);
+    err = launch_kernel(kvx_verify_walk_kernel<kType, true>, R, kWalk, stream, a);
+    if (!err) err = launch_kernel(kvx_verify_residual_kernel<kType>, residual_groups(a), kWg, stream, a);
+    if (!err) err = launch_kernel(kvx_verify_draw_kernel<kType>, R, kWalk, stream, a);
     return err;
 }
 
 }  // namespace
 
-bool verify_coarse(int64_t tokens, int32_t vocab, bool draft) { return tokens * vocab * (draft ? 2 : 1) >= 1 << 24; }
-
 double verify_threads(const VerifyArgs& a)
 {
-    double most = std::max(double(part_groups(a, std::max(a.total_tokens, a.num_requests))) * kWg,
-                           double(a.num_requests) * kWalk);
+    double most = std::max(double(part_groups(a)) * kWg, double(a.num_requests) * kWalk);
     if (a.draft) most = std::max(most, double(residual_groups(a)) * kWg);
     if (a.draft && a.parents) most = std::max(most, double(a.total_tokens) * kWalk);
     return most;

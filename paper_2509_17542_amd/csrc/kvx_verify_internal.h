@@ -37,14 +37,10 @@ struct VerifyArgs {
     int32_t a_stride, pad;
     // workspace
     Part* part[2];                       // [N][parts] of the target's and the draft's rows
-    Part* last_part[2];                  // [R][parts]: of the last tokens' rows; NULL: those of `part`
     double* left;                        // [N]: 1 / sum of what a token's refusal leaves of r
     double* residual;                    // [R][parts]: sums of r after the last token
-    int32_t* last;                       // [R]: it, -1: none
+    int32_t* last;                       // [R]: it (kLeaf: a leaf), -1: none; with a draft
 };
-
-// Whether the parts of all rows are summed in 32 bits and those of the last tokens' rows alone in 64 again.
-bool verify_coarse(int64_t tokens, int32_t vocab, bool draft);
 
 // Enqueues the kernels of a call; returns a hipError_t value.
 int launch_verify(const VerifyArgs& a, int dtype, void* stream);

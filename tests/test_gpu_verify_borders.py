@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_verify import TORCH, int32
+from test_gpu_verify import KINDS, TORCH, Problem, int32
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,38 @@ def test_accepted(K, distance, dtype):
     for draft in (None, sure):
         counts, _ = verify(K, logits, [0, 1] * 60, 2, [t for t, _, _ in near], u, [0.5] * 60, draft)
         assert counts == [2 if below else 1 for _, _, below in near]
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_accepted_in_a_large_call(K, dtype):
+    """The same decisions among 2^24 logits and more: as in a call of the request alone."""
+    vocab, distance, many = 20001, 10.0, 420
+    near = near_borders(distance, vocab, many, 3e-13, 5, True)
+    logits = torch.zeros((2 * many, vocab), dtype=TORCH[dtype], device="cuda")
+    assert logits.numel() >= 1 << 24
+    logits[:, 0] += distance
+    t, u = [t for t, _, _ in near], sum(([0.0, s] for _, s, _ in near), [])
+    counts, nxt = verify(K, logits, [0, 1] * many, 2, t, u, [0.7] * many)
+    assert counts == [2 if below else 1 for _, _, below in near]
+    for r in range(0, many, 30):
+        alone = verify(K, logits[2 * r:2 * r + 2], [0, 1], 2, t[r:r + 1], u[2 * r:2 * r + 2], [0.7])
+        assert alone == (counts[r:r + 1], nxt[r:r + 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+def test_alone_and_among_others(K, kind, dtype):
+    """A request's path and next token do not depend on how many others are in the call."""
+    new = [6, 30, 1, 16, 24, 9, 30]
+    p = Problem(new, vocab=150001, dtype=dtype, seed=31, near=0.97, peak=15.0, **kind)
+    assert p.logits.numel() >= 1 << 24
+    p.check(K)
+    _, counts, nxt = p.run(K)
+    for r in (0, 2, 5):
+        a, b = p.starts[r], p.starts[r + 1]
+        one = Problem([new[r]], vocab=4, dtype=dtype, seed=1, **kind)
+        one.vocab, one.tokens, one.parents = p.vocab, p.tokens[a:b], None if p.parents is None else p.parents[a:b]
+        one.d_logits, one.d_draft = p.d_logits[a:b], None if p.draft is None else p.d_draft[a:b]
+        one.uniforms, one.samples = p.uniforms[a:b], p.samples[r:r + 1]
+        _, c, n = one.run(K)
+        assert (int(c), int(n)) == (int(counts[r]), int(nxt[r]))

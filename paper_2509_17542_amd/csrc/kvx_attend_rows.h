@@ -69,7 +69,8 @@ struct Shape {
     static constexpr int kRing = 2 * kBatch;
 };
 
-template <bool kBf16, int kCodes, int DP, int NW, int kScores>
+// kRest: weights go into the product in two terms
+template <bool kBf16, int kCodes, int DP, int NW, int kScores, bool kRest>
 __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_kernel(const AttendArgs a, int row_tiles)
 {
     using S = Shape<kCodes, DP, NW>;
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
             }
             by_lift = __builtin_amdgcn_exp2f(lift);
         }
-        u32x4 pf[ST][2], rest[kTwo ? ST : 1][2];
+        u32x4 pf[ST][2], rest[kRest ? ST : 1][2];
 #pragma unroll
         for (int e = 0; e < ST; ++e)
 #pragma unroll
@@ -504,7 +505,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 u32x4& f = pf[e][b >> 1];
                 f[w] = pack2<kMath>(p[0], p[1]);
                 f[w + 1] = pack2<kMath>(p[2], p[3]);
-                if constexpr (kTwo) {
+                if constexpr (kRest) {
                     u32x4& g = rest[e][b >> 1];
                     g[w] = pack2<true>(p[0] - value16<true>(f[w] & 0xFFFFu), p[1] - value16<true>(f[w] >> 16));
                     g[w + 1] = pack2<true>(p[2] - value16<true>(f[w + 1] & 0xFFFFu), p[3] - value16<true>(f[w + 1] >> 16));
@@ -518,7 +519,7 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
                 for (int t2 = 0; t2 < DTB; ++t2) {
                     const u32x4 f = *reinterpret_cast<const u32x4*>(vl + t2 * 32 * S::kVRow + e * 64 + (b ^ (t2 & 1)) * 32);
                     o[t2] = mfma32<kMath>(f, pf[e][b], o[t2]);
-                    if constexpr (kTwo) o[t2] = mfma32<kMath>(f, rest[e][b], o[t2]);
+                    if constexpr (kRest) o[t2] = mfma32<kMath>(f, rest[e][b], o[t2]);
                 }
     };
 
@@ -661,24 +662,40 @@ __global__ void __launch_bounds__(64 * NW, (DP >= 256 ? 1 : 2)) kvx_attend_rows_
     }
 }
 
-template <bool kBf16, int kCodes, int DP, int NW, int kScores>
+template <bool kBf16, int kCodes, int DP, int NW, int kScores, bool kRest>
 int go_as(const AttendArgs& a, const AttendPlan& p, void* stream)
 {
     const int64_t groups = int64_t(a.c.num_requests) * a.splits * a.c.hd;
-    return launch_kernel(kvx_attend_rows_kernel<kBf16, kCodes, DP, NW, kScores>, groups * p.row_tiles, 64 * NW,
+    return launch_kernel(kvx_attend_rows_kernel<kBf16, kCodes, DP, NW, kScores, kRest>, groups * p.row_tiles, 64 * NW,
                          stream, a, p.row_tiles);
 }
 
+template <bool kBf16, int kCodes, int DP, int NW, bool kRest>
+int go_by(const AttendArgs& a, const AttendPlan& p, void* stream)
+{
+    switch (scores_of(a)) {
+    case kWide: return go_as<kBf16, kCodes, DP, NW, kCappedWide, kRest>(a, p, stream);
+    case kGeneral:
+        return a.softcap > 0.0f ? go_as<kBf16, kCodes, DP, NW, kCapped, kRest>(a, p, stream)
+                                : go_as<kBf16, kCodes, DP, NW, kBiased, kRest>(a, p, stream);
+    default: return go_as<kBf16, kCodes, DP, NW, kPlain, kRest>(a, p, stream);
+    }
+}
+
+// Weights in two terms: over 4 bits of fp16 queries, whose bits one bf16 does not hold, and of calls
+// of up to 16 rows, which come here where the few-rows kernel cannot number the groups.
 template <bool kBf16, int kCodes, int DP, int NW>
 int go(const AttendArgs& a, const AttendPlan& p, void* stream)
 {
-    switch (scores_of(a)) {
-    case kWide: return go_as<kBf16, kCodes, DP, NW, kCappedWide>(a, p, stream);
-    case kGeneral:
-        return a.softcap > 0.0f ? go_as<kBf16, kCodes, DP, NW, kCapped>(a, p, stream)
-                                : go_as<kBf16, kCodes, DP, NW, kBiased>(a, p, stream);
-    default: return go_as<kBf16, kCodes, DP, NW, kPlain>(a, p, stream);
-    }
+    if constexpr (kCodes != kCodesE2m1)
+        return go_by<kBf16, kCodes, DP, NW, false>(a, p, stream);
+    else if constexpr (!kBf16)
+        return go_by<kBf16, kCodes, DP, NW, true>(a, p, stream);
+    else if constexpr (NW == 2)
+        return p.rows <= 16 ? go_by<kBf16, kCodes, DP, NW, true>(a, p, stream)
+                            : go_by<kBf16, kCodes, DP, NW, false>(a, p, stream);
+    else
+        return go_by<kBf16, kCodes, DP, NW, false>(a, p, stream);
 }
 
 template <bool kBf16, int kCodes>

@@ -283,24 +283,24 @@ __device__ __forceinline__ double share(float l, float top, double rate, double 
     return exp2_256th(table, (double(l) - double(top)) * rate) * by;
 }
 
-// What refusing k children leaves of one element's r; q0 is its share of the draft's row.
-// Child j has the token x(j), q divided by cq(j), and r multiplied by left(j) after it.
-template <typename X, typename C, typename L>
-__device__ __forceinline__ double refused(double r, double q0, int v, int k, bool distinct, X x, C cq, L left)
+// What refusing children leaves of r.  Child j's refusal makes r(v) left(j) max(r(v) - q(v) by(j), 0), the
+// factor `left` bringing its sum to 1, from r = p on.  All of them come to one term:
+//   r(v) = A max(p(v) - q(v) B, 0),   A = left(0) .. left(j),
+//   B = by(0) + by(1) / left(0) + .. + by(j) / (left(0) .. left(j - 1)),
+// since max(A max(x, 0) - y, 0) = A max(x - y / A, 0) for positive A and y.  Siblings drawn without
+// replacement take their tokens out of q: of child i's token B ends with by(i).  So a refusal's pass over
+// a row takes the same work whatever the number of children (a token's children times V in all;
+// replaying the refusals before each took 59 ms for 128 children and 32000 logits, 1.6 so).
+__device__ __forceinline__ double rest(double p, double q, double upto)
 {
-    bool gone = false;
-    for (int j = 0; j < k; ++j) {
-        r = fmax(r - (gone ? 0.0 : q0 * cq(j)), 0.0) * left(j);
-        gone |= distinct && x(j) == v;
-    }
-    return r;
+    return fmax(__builtin_fma(-upto, q, p), 0.0);
 }
 
 // The children of a token, in LDS: their numbers, tokens, and the factors above.
 struct Children {
     int number[kMaxDrafted];
     int token[kMaxDrafted];
-    double by[kMaxDrafted];              // what q is multiplied by at that child
+    double by[kMaxDrafted];              // what q is multiplied by at that child; then the B above up to it
     double left[kMaxDrafted];
     uint8_t dull[kMaxDrafted];           // a token that an earlier sibling is, or none of the vocabulary
     int count;
@@ -370,6 +370,17 @@ __device__ __forceinline__ double group_sum(double x, double* s_part)
     return sum;
 }
 
+// What child j's token has more than rest(p, q, upto), its B having ended with by(j).
+template <int kType>
+__device__ __forceinline__ double own_token(const char* pr, const char* qr, const Whole& p, const Whole& q, double rate,
+                                            double ip, double iq, const double* table, const Children& s, int j, double upto)
+{
+    if (s.dull[j]) return 0.0;
+    const double a = share(logit<kType>(pr, s.token[j]), p.top, rate, ip, table);
+    const double b = share(logit<kType>(qr, s.token[j]), q.top, rate, iq, table);
+    return rest(a, b, s.by[j]) - rest(a, b, upto);
+}
+
 // ---- siblings --------------------------------------------------------------------
 
 // A workgroup per token with several children: what the refusal of each but the last leaves.
@@ -410,22 +421,22 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_siblings_kernel(const Verify
     };
     draft_factors<kType>(a, qr, q, rate, s_table, s_kids);
     const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;
+    double scale = 1.0, upto = 0.0;                    // A and B
     for (int k = 0; k + 1 < count; ++k) {
-        if (threadIdx.x == 0) s_kids.left[k] = 1.0;
-        __syncthreads();
-        auto one = [&](float lp, float lq, int v) {
-            return refused(share(lp, p.top, rate, ip, s_table), share(lq, q.top, rate, iq, s_table), v, k + 1,
-                           a.distinct, [&](int j) { return s_kids.token[j]; }, [&](int j) { return s_kids.by[j]; },
-                           [&](int j) { return s_kids.left[j]; });
-        };
+        upto += s_kids.by[k] / scale;
         double sum = 0.0;
-        walk([&](float lp, float lq, int v) { sum += one(lp, lq, v); });
+        walk([&](float lp, float lq, int) {
+            sum += rest(share(lp, p.top, rate, ip, s_table), share(lq, q.top, rate, iq, s_table), upto);
+        });
+        if (a.distinct)
+            for (int j = int(threadIdx.x); j < k; j += kWalk) sum += own_token<kType>(pr, qr, p, q, rate, ip, iq, s_table, s_kids, j, upto);
         sum = group_sum<kWalk>(sum, s_part);
+        const double left = sum > 0x1p-1000 ? 1.0 / (scale * sum) : 1.0;
         if (threadIdx.x == 0) {
-            const double left = sum > 0.0 ? 1.0 / sum : 1.0;
-            s_kids.left[k] = left;
+            s_kids.by[k] = upto;
             a.left[d.first + s_kids.number[k]] = left;
         }
+        scale *= left;
         __syncthreads();
     }
 }
@@ -707,9 +718,16 @@ __device__ __forceinline__ bool last_row(const VerifyArgs& a, int r, double* tab
     if (count > 0) {
         q = join(a.part[1] + row * a.parts, a.parts, rate, table, lane, 64);
         draft_factors<kType>(a, row_of(a, 1, row, kSize<kType>), q, rate, table, kids);
-        // after the last refusal r needs no sum of 1
-        for (int j = int(threadIdx.x); j < count; j += int(blockDim.x))
-            kids.left[j] = j + 1 < count ? a.left[d.first + kids.number[j]] : 1.0;
+        for (int j = int(threadIdx.x); j + 1 < count; j += int(blockDim.x)) kids.left[j] = a.left[d.first + kids.number[j]];
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            double scale = 1.0, upto = 0.0;
+            for (int j = 0; j < count; ++j) {
+                upto += kids.by[j] / scale;
+                kids.by[j] = upto;
+                if (j + 1 < count) scale *= kids.left[j];
+            }
+        }
     }
     __syncthreads();
     return true;
@@ -741,20 +759,24 @@ __global__ void __launch_bounds__(kWg) kvx_verify_residual_kernel(const VerifyAr
             sum = t.sum * exp2_256th(s_table, (double(t.top) - double(p.top)) * rate);
     } else {
         const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;
-        auto one = [&](float lp, float lq, int v) {
-            return refused(share(lp, p.top, rate, ip, s_table), share(lq, q.top, rate, iq, s_table), c * kPart + v, count,
-                           a.distinct, [&](int j) { return s_kids.token[j]; }, [&](int j) { return s_kids.by[j]; },
-                           [&](int j) { return s_kids.left[j]; });
+        // after the last refusal r needs no sum of 1
+        const double upto = s_kids.by[count - 1];
+        auto one = [&](float lp, float lq) {
+            return rest(share(lp, p.top, rate, ip, s_table), share(lq, q.top, rate, iq, s_table), upto);
         };
         for (int v = lane * kV; v < n; v += 64 * kV) {
             if (v + kV <= n) {
                 const u32x4 s = load16(x + v * kSize<kType>), t = load16(y + v * kSize<kType>);
 #pragma unroll
-                for (int e = 0; e < kV; ++e) sum += one(element<kType>(s, e), element<kType>(t, e), v + e);
+                for (int e = 0; e < kV; ++e) sum += one(element<kType>(s, e), element<kType>(t, e));
             } else {
-                for (int e = v; e < n; ++e) sum += one(logit<kType>(x, e), logit<kType>(y, e), e);
+                for (int e = v; e < n; ++e) sum += one(logit<kType>(x, e), logit<kType>(y, e));
             }
         }
+        if (a.distinct)
+            for (int j = lane; j + 1 < count; j += 64)
+                if (s_kids.token[j] / kPart == c)
+                    sum += own_token<kType>(x - from, y - from, p, q, rate, ip, iq, s_table, s_kids, j, upto);
     }
     sum = wave_sum(sum);
     if (lane == 0) a.residual[int64_t(r) * a.parts + c] = sum;
@@ -780,10 +802,14 @@ __global__ void __launch_bounds__(kWalk) kvx_verify_draw_kernel(const VerifyArgs
         a, sample, s_scan, s_pick, [&](int c) { return a.residual[int64_t(r) * a.parts + c]; },
         [&](int v) {
             if (count == 0) return share(logit<kType>(x, v), p.top, rate, 1.0, s_table);
-            return refused(share(logit<kType>(x, v), p.top, rate, ip, s_table),
-                           share(logit<kType>(y, v), q.top, rate, iq, s_table), v, count, a.distinct,
-                           [&](int j) { return s_kids.token[j]; }, [&](int j) { return s_kids.by[j]; },
-                           [&](int j) { return s_kids.left[j]; });
+            double upto = s_kids.by[count - 1];
+            for (int j = 0; j < count && a.distinct; ++j)
+                if (s_kids.token[j] == v) {
+                    upto = s_kids.by[j];
+                    break;
+                }
+            return rest(share(logit<kType>(x, v), p.top, rate, ip, s_table),
+                        share(logit<kType>(y, v), q.top, rate, iq, s_table), upto);
         });
     if (next < 0)
         next = draw_plain<kType>(a, x, a.part[0] + row * a.parts, p, rate, s_kids.number, 0, sample, s_table, s_scan, s_pick);

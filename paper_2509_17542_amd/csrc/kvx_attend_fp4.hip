@@ -28,10 +28,11 @@
 // the beginning of the next one is two segments; a segment that is not all of its request leaves
 // its sums for kvx_fp4_join_kernel.  Requests of up to 1024 slots have a workgroup each.
 //
-// Those 64 requests (8 KV heads of 4 query heads, 128 elements, 311 MB) take 72 us and the join
-// 5: 4.0 TB/s in all; the turns by themselves, with nothing done to the rows, 47 (6.0 TB/s, as a
-// plain stream of 128-byte pieces at strides of 512), the rest is the chains at a range's
-// ends.  The many-rows kernel takes 183.  One request of 120000 slots, fp16, 4 KV heads: 30.
+// Those 64 requests (8 KV heads of 4 query heads, 128 elements, 311 MB) take 73 us and the join
+// 5: 4.0 TB/s in all.  With nothing done to the rows once they are there it is 71: what bounds it
+// are the loads and, at a range's ends, chains of them (lengths, table, scale bytes, first rows).  A lane
+// holds two tiles of rows: 211 registers of 256, fp16 queries 228.  The many-rows kernel takes 183.  One
+// request of 120000 slots, fp16, 4 KV heads: 30.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -794,7 +795,10 @@ void plan_few_fp4(const kvx_cache& c, const kvx_batch& b, AttendPlan& p)
     p.heads = c.head_dim > 128 ? 1 : c.head_dim > 64 ? 2 : 4;
     while (p.heads > 1 && (c.num_kv_heads % p.heads || p.rows * p.heads > 8)) p.heads >>= 1;
     // A workgroup to each request's pack: short ones, and so many that the card evens them out and
-    // finding a range's place among them would cost; fewer heads to each where they do not fill the card.
+    // finding a range's place among them would cost (8 KV heads of 4 query heads, 128 elements: 512 requests of
+    // 1100..1300 slots 159 us, 193 in ranges, of 500..4000 294 and 308; 256 of 500..4000 174 and 164).  Where
+    // one of so many is far longer than the others it is what a call takes: 60000 slots among 511 requests of
+    // 1000 808 us, 184 in ranges; the host does not know lengths.  Fewer heads to each where they do not fill the card.
     const int64_t requests = c.num_requests, turns = (int64_t(b.max_context) + kStep - 1) / kStep;
     const bool single = turns <= 8 || requests >= 512 || requests * (c.num_kv_heads / p.heads) >= 1024;
     while (single && p.heads > 1 && requests * (c.num_kv_heads / p.heads) < 256) p.heads >>= 1;

@@ -683,7 +683,9 @@ int go_by(const AttendArgs& a, const AttendPlan& p, void* stream)
 }
 
 // Weights in two terms: over 4 bits of fp16 queries, whose bits one bf16 does not hold, and of calls
-// of up to 16 rows, which come here where the few-rows kernel cannot number the groups.
+// of up to 16 rows, which come here where the few-rows kernel cannot number the groups.  Other bf16
+// calls round them once, as over the other caches (16 trees of 16..64 nodes 252 us, 281 with two terms;
+// two chunks of 512..1024 tokens with a bias, a window and a prefix 361, 411).
 template <bool kBf16, int kCodes, int DP, int NW>
 int go(const AttendArgs& a, const AttendPlan& p, void* stream)
 {

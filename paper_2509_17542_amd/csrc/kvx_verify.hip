@@ -14,9 +14,9 @@
 // The next token is the place where a sum over up to V terms passes a given share of
 // the whole: an error of 1e-7 of it, as of fp32 exponentials, moves thousands of such
 // borders by that much, so all sums are of 64 bits, from exponentials of 2e-13, and a
-// request has the same answer in a call of any size.  80 million logits of bf16 take 68 us, 2.4
+// request has the same answer in a call of any size.  80 million logits of bf16 take 67 us, 2.4
 // TB/s (41 with fp32 exponentials, summed eight at a time in fp32).
-// 64 chains of 2..9 tokens over 128256 logits with a draft's take 123 us, four tokens over 32000
+// 64 chains of 2..9 tokens over 128256 logits with a draft's take 110 us, four tokens over 32000
 // logits 21, nearly all of it launches and chains of lookups.
 #include <hip/hip_runtime.h>
 
